@@ -555,7 +555,8 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *s
     const int cols = MODE == FORWARD ? a.Dv : ws.cols;
     auto go = [&](auto dk, auto ns) {
         constexpr int DK = decltype(dk)::value, NS = decltype(ns)::value, W = 16 * NS;
-        const bool full = a.Dk == DK && a.Dv % W == 0 && full_rows<E>(a.q, DK, q) && full_rows<E>(a.k, DK, k) && full_rows<E>(a.v, W, v) &&
+        // (every block of columns that the grid has must be one of the values: whole loads do not stop at the end of a head)
+        const bool full = a.Dk == DK && a.Dv == cols && cols % W == 0 && full_rows<E>(a.q, DK, q) && full_rows<E>(a.k, DK, k) && full_rows<E>(a.v, W, v) &&
                           full_rows<E>(a.o, W, o);
         auto *kernel = full ? delta_scan_kernel<E, DK, NS, MODE, true> : delta_scan_kernel<E, DK, NS, MODE, false>;
         static std::atomic<uint64_t> raised[2] = {{0}, {0}};

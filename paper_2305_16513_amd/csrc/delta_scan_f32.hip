@@ -227,11 +227,11 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *s
     if (heads > 0x7fffffff) return kNotTaken;
     auto go = [&](auto dk, auto nw) {
         constexpr int DK = decltype(dk)::value, NW = decltype(nw)::value;
-        const bool full = a.Dk == DK && a.Dv % (16 * NW) == 0 && full_rows<E>(a.q, DK, q) && full_rows<E>(a.k, DK, k) && full_rows<E>(a.v, 16 * NW, v) &&
-                          full_rows<E>(a.o, 16 * NW, o);
-        auto *kernel = full ? delta_scan_kernel<E, DK, NW, MODE, true> : delta_scan_kernel<E, DK, NW, MODE, false>;
         // the gradients read whole blocks of 32 columns of what is kept
         const int cols = MODE == FORWARD ? a.Dv : ws.cols;
+        const bool full = a.Dk == DK && a.Dv == cols && cols % (16 * NW) == 0 && full_rows<E>(a.q, DK, q) && full_rows<E>(a.k, DK, k) && full_rows<E>(a.v, 16 * NW, v) &&
+                          full_rows<E>(a.o, 16 * NW, o);
+        auto *kernel = full ? delta_scan_kernel<E, DK, NW, MODE, true> : delta_scan_kernel<E, DK, NW, MODE, false>;
         const dim3 grid((unsigned)heads, (unsigned)((cols + 16 * NW - 1) / (16 * NW)));
         hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, s, (const E *)q, (const E *)k, (const E *)v, (E *)o, state, ws, a);
         return hipGetLastError();
