@@ -6,13 +6,14 @@
     o = delta_rule(q, k, v, g, beta)     g = -exp(rate) softplus(a + offset),  beta = sigmoid(b)
     x = norm_gate(o, z) W'
 
-Training goes through torch's autograd, with the operators' own gradients.  Serving reads and writes the sequences' places in two pools per block: the tokens in front of
+Training goes through torch's autograd, with the operators' own gradients (once: second derivatives raise).  Serving reads and writes the sequences' places in two pools per block: the tokens in front of
 the next one, and the state.  A prompt and a single token are the same call.
 
     python -m paper_2305_16513_amd.delta_layer      # trains a model to go on with a pattern, then lets it, from prompts of several lengths
 """
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 from torch.nn import functional as F
 
 from . import binding as B
@@ -30,6 +31,7 @@ class _NormAdd(torch.autograd.Function):
         return n if x is None else (h, n)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, *grads):
         r, w, x, gain = ctx.saved_tensors
         gh, gn = (None, grads[0]) if x is None else grads
@@ -45,6 +47,7 @@ class _ShortConv(torch.autograd.Function):
         return B.sws_short_conv(x, w, **ctx.how)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         gx, gw, gbias = B.sws_short_conv_grad(*ctx.saved_tensors, gy.contiguous(), **ctx.how)
         return gx, gw, gbias, None, None
@@ -60,6 +63,7 @@ class _DeltaRule(torch.autograd.Function):
         return B.sws_delta_rule(*parts(row), g, beta)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, go):
         row, g, beta = ctx.saved_tensors
         grow = torch.empty_like(row)
@@ -75,6 +79,7 @@ class _NormGate(torch.autograd.Function):
         return B.sws_norm_gate(x, z, w, EPS)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         x, z, w = ctx.saved_tensors
         return B.sws_norm_gate_grad(x, z, w, gy.contiguous(), EPS)
