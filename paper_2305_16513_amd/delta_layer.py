@@ -42,14 +42,15 @@ class _NormAdd(torch.autograd.Function):
 class _ShortConv(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, unit, unit_channels):
-        ctx.how = dict(bias=bias, act=B.SWS_ACT_SILU, unit=unit, unit_channels=unit_channels, eps=EPS)
-        ctx.save_for_backward(x, w)
-        return B.sws_short_conv(x, w, **ctx.how)
+        ctx.how = dict(act=B.SWS_ACT_SILU, unit=unit, unit_channels=unit_channels, eps=EPS)
+        ctx.save_for_backward(x, w, bias)
+        return B.sws_short_conv(x, w, bias=bias, **ctx.how)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, gy):
-        gx, gw, gbias = B.sws_short_conv_grad(*ctx.saved_tensors, gy.contiguous(), **ctx.how)
+        x, w, bias = ctx.saved_tensors
+        gx, gw, gbias = B.sws_short_conv_grad(x, w, gy.contiguous(), bias=bias, **ctx.how)
         return gx, gw, gbias, None, None
 
 

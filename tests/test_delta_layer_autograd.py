@@ -79,3 +79,21 @@ def test_second_derivatives_are_refused(plain):
         grads = torch.autograd.grad(sum(o.square().sum() for o in outs), ins, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             sum(g.square().sum() for g in grads).backward()
+
+
+def test_whatever_the_gradients_read_is_saved(plain):
+    """An input that is changed in place between a call and its gradients is an error, and hooks on saved tensors see every one."""
+    gen = torch.Generator().manual_seed(3)
+    for which, (f, args) in enumerate(_operators(gen)):
+        ins = [a for a in args if isinstance(a, torch.Tensor)]
+        for i in range(len(ins)):
+            seen = []
+            with torch.autograd.graph.saved_tensors_hooks(lambda t: seen.append(t.data_ptr()) or t, lambda t: t):
+                out = f.apply(*args)
+            assert ins[i].data_ptr() in seen, (which, i)
+            out = f.apply(*args)
+            out = out if isinstance(out, tuple) else (out,)
+            with torch.no_grad():
+                ins[i].mul_(2)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                sum(o.sum() for o in out).backward()
