@@ -117,6 +117,10 @@ class DeltaBlock(nn.Module):
     def forward(self, h, x=None, cache=None, slots=None, lengths=None):
         """h, and x that has yet to join it, [B, T, width] -> the new h, x.  With a cache: the next T tokens (lengths: so many of them) of the sequences at `slots`, without
         gradients."""
+        with torch.set_grad_enabled(torch.is_grad_enabled() and cache is None):
+            return self._next(h, x, cache, slots, lengths)
+
+    def _next(self, h, x, cache, slots, lengths):
         if x is None:
             n = _NormAdd.apply(h, self.norm, None, None)
         else:
@@ -145,11 +149,12 @@ class DeltaModel(nn.Module):
         self.head = nn.Linear(width, symbols, bias=False, dtype=dtype, device=device)
 
     def forward(self, tokens, caches=None, slots=None, lengths=None):
-        """tokens [B, T] -> logits [B, T, symbols] in fp32"""
-        h, x = self.table(tokens), None
-        for i, block in enumerate(self.blocks):
-            h, x = block(h, x, caches and caches[i], slots, lengths)
-        return self.head(_NormAdd.apply(h, self.norm, x, self.gain)[1]).float()
+        """tokens [B, T] -> logits [B, T, symbols] in fp32; with caches without gradients"""
+        with torch.set_grad_enabled(torch.is_grad_enabled() and caches is None):
+            h, x = self.table(tokens), None
+            for i, block in enumerate(self.blocks):
+                h, x = block(h, x, caches and caches[i], slots, lengths)
+            return self.head(_NormAdd.apply(h, self.norm, x, self.gain)[1]).float()
 
     def caches(self, places):
         return [Cache(block, places) for block in self.blocks]

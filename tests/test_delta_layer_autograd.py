@@ -97,3 +97,15 @@ def test_whatever_the_gradients_read_is_saved(plain):
                 ins[i].mul_(2)
             with pytest.raises(RuntimeError, match="modified by an inplace operation"):
                 sum(o.sum() for o in out).backward()
+
+
+def test_serving_has_no_gradients(plain):
+    """Calls with caches write them in place: what they return does not pretend to have gradients, of which some paths would be missing."""
+    torch.manual_seed(4)
+    m = D.DeltaModel(5, 8, 2, 1, 2, 4, 3, dtype=torch.float32, device="cpu")
+    tokens = torch.tensor([[1, 2, 3]])
+    assert m(tokens).requires_grad
+    assert not m(tokens, m.caches(1)).requires_grad
+    h, x = m.blocks[0](m.table(tokens), cache=m.caches(1)[0])
+    assert not x.requires_grad
+    assert torch.is_grad_enabled()
