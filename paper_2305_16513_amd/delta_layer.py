@@ -171,7 +171,7 @@ class DeltaModel(nn.Module):
         out = [last.argmax(-1)]
         for _ in range(count - 1):
             out.append(self(out[-1][:, None], caches, slots)[:, -1].argmax(-1))
-        return torch.stack(out, 1).tolist()
+        return torch.stack(out, 1)[:, :count].tolist()
 
 
 def patterns(generator, batch, length, symbols, shortest=3, longest=9):

@@ -109,3 +109,8 @@ def test_serving_has_no_gradients(plain):
     h, x = m.blocks[0](m.table(tokens), cache=m.caches(1)[0])
     assert not x.requires_grad
     assert torch.is_grad_enabled()
+
+
+def test_no_symbols_are_asked_for(plain):
+    m = D.DeltaModel(5, 8, 1, 1, 2, 4, 3, dtype=torch.float32, device="cpu")
+    assert m.answer([[1], [2, 3]], 0) == [[], []] and [len(a) for a in m.answer([[1], [2, 3]], 2)] == [2, 2]
