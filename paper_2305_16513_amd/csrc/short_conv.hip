@@ -45,8 +45,9 @@ __device__ __forceinline__ Place place_of(const ShortConvArgs &a)
     Place p;
     const int per = kThreads / a.lanes, group = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
     p.head = blockIdx.x * per + group;
-    p.run = blockIdx.y % a.runs;
-    p.b = (int64_t)blockIdx.z * 32768 + blockIdx.y / a.runs;
+    const unsigned at = blockIdx.z * gridDim.y + blockIdx.y;      // (the last of z may reach beyond the last sequence)
+    p.run = at % a.runs;
+    p.b = at / a.runs;
     p.live = p.head < a.heads;
     p.c0 = p.head * a.unit + 8 * lane;
     const int in_head = a.unit - 8 * lane, in_row = a.C - p.c0;
@@ -333,13 +334,14 @@ void plan(ShortConvArgs &a, int unit, int unit_channels, int slots)
     a.runs = (int)((a.T + a.run - 1) / a.run);
 }
 
+// Runs of all sequences in y and z, at most 65535 in each
 bool grid_of(const ShortConvArgs &a, dim3 &grid)
 {
     const int per = kThreads / a.lanes;
-    const int64_t gx = (a.heads + per - 1) / per;
-    const int64_t b = a.B < 32768 ? a.B : 32768, gz = (a.B + 32767) / 32768;
-    if (a.B * a.runs > 0x7fffffff || gz > 65535) return false;
-    grid = dim3((unsigned)gx, (unsigned)(b * a.runs), (unsigned)gz);
+    const int64_t gx = (a.heads + per - 1) / per, n = a.B * a.runs;
+    if (n > 0x7fffffff) return false;
+    const int64_t gz = (n + 65534) / 65535, gy = (n + gz - 1) / gz;
+    grid = dim3((unsigned)gx, (unsigned)gy, (unsigned)gz);
     return true;
 }
 
