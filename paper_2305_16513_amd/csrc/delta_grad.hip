@@ -72,8 +72,9 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), w = wave % 4, l = tid % 16, gr = tid % kWave / 16;
     const int th = w / 2, dh = w & 1;                 // tiles 2 th, 2 th + 1 of the tokens, KH dh ... of the keys' elements; w's own tile of tokens is 2 th + dh
     const bool second = wave >= 4;                    // M's wavefronts
-    const int c = blockIdx.x % ws.chunks;
-    const int64_t unit = blockIdx.x / ws.chunks, b = unit / a.Hk;
+    const int64_t unit = group_of() / (unsigned)ws.chunks, b = (unsigned)unit / (unsigned)a.Hk;
+    const int c = group_of() % (unsigned)ws.chunks;
+    if (b >= a.B) return;
     const int hk = (int)(unit - b * a.Hk), share = a.Hv / a.Hk;
     const int64_t t0 = (int64_t)c * kChunk, left = tokens_of(a, b) - t0;
     const int n = left <= 0 ? 0 : left < kChunk ? (int)left : kChunk;
@@ -482,15 +483,15 @@ hipError_t launch_delta_grad(int dtype, int gate_dtype, const void *q, const voi
                              void *gk, void *gv, void *gg, void *gbeta, const void *u, const void *r, const void *st, const void *ds, int chunks, int cols,
                              bool full, const DeltaArgs &a, const Steps (&gs)[3], hipStream_t s)
 {
-    const int64_t grid = a.B * a.Hk * chunks;
-    if (grid > 0x7fffffff) return kNotTaken;
+    dim3 grid;
+    if (!spread(a.B * a.Hk * chunks, kThreads, grid)) return kNotTaken;
     const GradWs ws{u, r, st, ds, chunks, cols};
     return by_type(dtype, [&](auto *t) {
         using E = std::remove_pointer_t<decltype(t)>;
         auto with = [&](auto *x) {
             using G = std::remove_pointer_t<decltype(x)>;
             auto go_ = [&](auto *kernel) {
-                hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, (const E *)q, (const E *)k, (const E *)v, (const G *)g, (const G *)beta,
+                hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, (const E *)q, (const E *)k, (const E *)v, (const G *)g, (const G *)beta,
                                    (const E *)go, (E *)gq, (E *)gk, (E *)gv, (G *)gg, (G *)gbeta, ws, a, gs[0], gs[1], gs[2]);
                 return hipGetLastError();
             };

@@ -56,8 +56,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
     const Keys at;
     __shared__ double sums[kChunk];
     __shared__ float betas[kChunk];
-    const int c = blockIdx.x % chunks, w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int64_t head = blockIdx.x / chunks, b = head / a.Hv;
+    const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t head = group_of() / (unsigned)chunks, b = (unsigned)head / (unsigned)a.Hv;
+    const int c = group_of() % (unsigned)chunks;
+    if (b >= a.B) return;
     const int h = (int)(head - b * a.Hv), hk = h / (a.Hv / a.Hk);
     const int64_t t0 = (int64_t)c * kChunk, left = tokens_of(a, b) - t0;
     if (left <= 0) return;
@@ -197,14 +199,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
 hipError_t launch_delta_prep(int dtype, int gate_dtype, const void *q, const void *k, const void *g, const void *beta, char *tri, float *factors, int chunks,
                              bool full, bool grad, const DeltaArgs &a, hipStream_t s)
 {
-    const int64_t grid = a.B * a.Hv * chunks;
-    if (grid > 0x7fffffff) return kNotTaken;
+    dim3 grid;
+    if (!spread(a.B * a.Hv * chunks, 256, grid)) return kNotTaken;
     return by_type(dtype, [&](auto *t) {
         using E = std::remove_pointer_t<decltype(t)>;
         auto with = [&](auto *u) {
             using G = std::remove_pointer_t<decltype(u)>;
             auto go = [&](auto *kernel) {
-                hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, s, (const E *)q, (const E *)k, (const G *)g, (const G *)beta, tri, factors, chunks,
+                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const E *)q, (const E *)k, (const G *)g, (const G *)beta, tri, factors, chunks,
                                    a);
                 return hipGetLastError();
             };

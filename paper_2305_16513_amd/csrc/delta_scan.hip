@@ -76,7 +76,8 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
     auto &fs = m.fs;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), w = wave % NS, hf = wave / NS % 2, lane = threadIdx.x % kWave, l = lane % 16,
               gr = lane / 16;
-    const int64_t head = blockIdx.x, b = head / a.Hv;
+    const int64_t head = group_of(), b = group_of() / (unsigned)a.Hv;
+    if (b >= a.B) return;
     const int h = (int)(head - b * a.Hv), hk = h / (a.Hv / a.Hk);
     const int col0 = blockIdx.y * W;                  // the workgroup's first column of the state
     int64_t len = tokens_of(a, b);
@@ -550,7 +551,6 @@ template <class E, int MODE>
 hipError_t launch(const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws, const DeltaArgs &a, hipStream_t s)
 {
     const int64_t heads = a.B * a.Hv;
-    if (heads > 0x7fffffff) return kNotTaken;
     // the gradients read whole blocks of 32 columns of what is kept
     const int cols = MODE == FORWARD ? a.Dv : ws.cols;
     auto go = [&](auto dk, auto ns) {
@@ -562,7 +562,9 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *s
         static std::atomic<uint64_t> raised[2] = {{0}, {0}};
         constexpr int bytes = sizeof(ScanLds<E, DK, NS, MODE>);
         if (const hipError_t e = raise_lds((const void *)kernel, bytes, raised[full])) return e;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)heads, (unsigned)((cols + W - 1) / W)), dim3(scan_threads(NS, MODE)), bytes, s, (const E *)q, (const E *)k, (const E *)v,
+        dim3 grid;
+        if (!spread(heads, scan_threads(NS, MODE), grid, (unsigned)((cols + W - 1) / W))) return kNotTaken;
+        hipLaunchKernelGGL(kernel, grid, dim3(scan_threads(NS, MODE)), bytes, s, (const E *)q, (const E *)k, (const E *)v,
                            (E *)o, state, ws, a);
         return hipGetLastError();
     };

@@ -24,7 +24,8 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
     __shared__ __align__(16) v4u ts[TU];
     __shared__ __align__(16) float fs[3 * kChunk];
     const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave, l = lane % 16, gr = lane / 16;
-    const int64_t head = blockIdx.x, b = head / a.Hv;
+    const int64_t head = group_of(), b = group_of() / (unsigned)a.Hv;
+    if (b >= a.B) return;
     const int h = (int)(head - b * a.Hv), hk = h / (a.Hv / a.Hk);
     const int col0 = blockIdx.y * W;                  // the workgroup's first column of the state
     int64_t len = tokens_of(a, b);
@@ -224,7 +225,6 @@ template <class E, int MODE>
 hipError_t launch(const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws, const DeltaArgs &a, hipStream_t s)
 {
     const int64_t heads = a.B * a.Hv;
-    if (heads > 0x7fffffff) return kNotTaken;
     auto go = [&](auto dk, auto nw) {
         constexpr int DK = decltype(dk)::value, NW = decltype(nw)::value;
         // the gradients read whole blocks of 32 columns of what is kept
@@ -232,7 +232,8 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *s
         const bool full = a.Dk == DK && a.Dv == cols && cols % (16 * NW) == 0 && full_rows<E>(a.q, DK, q) && full_rows<E>(a.k, DK, k) && full_rows<E>(a.v, 16 * NW, v) &&
                           full_rows<E>(a.o, 16 * NW, o);
         auto *kernel = full ? delta_scan_kernel<E, DK, NW, MODE, true> : delta_scan_kernel<E, DK, NW, MODE, false>;
-        const dim3 grid((unsigned)heads, (unsigned)((cols + 16 * NW - 1) / (16 * NW)));
+        dim3 grid;
+        if (!spread(heads, 64 * NW, grid, (unsigned)((cols + 16 * NW - 1) / (16 * NW)))) return kNotTaken;
         hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, s, (const E *)q, (const E *)k, (const E *)v, (E *)o, state, ws, a);
         return hipGetLastError();
     };

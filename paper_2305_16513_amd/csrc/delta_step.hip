@@ -27,8 +27,9 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(const E *__restric
     __shared__ float qs[kTokens][DK], ks[kTokens][DK], gs[kTokens], bs[kTokens], qk[kTokens];
     __shared__ v4f sums[2][2][4][LANES];              // in turn; w and z; of each wavefront
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, wave = threadIdx.x / kWave;
-    const int64_t b = blockIdx.x / a.Hv;
-    const int h = (int)(blockIdx.x - b * a.Hv), hk = h / (a.Hv / a.Hk);
+    const int64_t head = group_of(), b = group_of() / (unsigned)a.Hv;
+    if (b >= a.B) return;
+    const int h = (int)(head - b * a.Hv), hk = h / (a.Hv / a.Hk);
     const int c0 = blockIdx.y * W + 4 * lane, left = a.Dv - c0;       // columns of this lane
     int64_t len = tokens_of(a, b);
     const int64_t slot = a.slots ? a.slots[b] : b;
@@ -147,9 +148,9 @@ hipError_t launch_delta_step(int dtype, int gate_dtype, const void *q, const voi
                              float *pool, const DeltaArgs &a, hipStream_t s)
 {
     const int64_t heads = a.B * a.Hv;
-    if (heads > 0x7fffffff) return kNotTaken;
     const bool wide = heads * ((a.Dv + 127) / 128) >= 2 * device_cus();
-    const dim3 grid((unsigned)heads, (unsigned)((a.Dv + (wide ? 127 : 31)) / (wide ? 128 : 32)));
+    dim3 grid;
+    if (!spread(heads, kThreads, grid, (unsigned)((a.Dv + (wide ? 127 : 31)) / (wide ? 128 : 32)))) return kNotTaken;
     const bool full = a.Dv % 4 == 0 && ((uintptr_t)pool & 15) == 0;
     return by_type(dtype, [&](auto *t) {
         using E = std::remove_pointer_t<decltype(t)>;

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void norm_add_kernel(const E *__restrict_
     __shared__ float lds[8];
     int turn = 0;
     const int lane = threadIdx.x % NT;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
+    const int64_t row = (int64_t)group_of() * (kThreads / NT) + threadIdx.x / NT;
     const bool live = row < a.rows;                   // (no return: shuffles and barriers are everybody's)
     const int64_t base = live ? row * a.width : 0;
     float v[NV][8], sum = 0;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void norm_gate_kernel(const E *__restrict
     __shared__ float lds[8];
     int turn = 0;
     const int lane = threadIdx.x % NT;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
+    const int64_t row = (int64_t)group_of() * (kThreads / NT) + threadIdx.x / NT;
     const bool live = row < a.rows;
     const int64_t token = live ? row / a.heads : 0;
     const int head = live ? (int)(row - token * a.heads) : 0;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float *__restri
 {
     __shared__ float lds[32][33];
     const int c = threadIdx.x % 32, g = threadIdx.x / 32;
-    const int64_t column = (int64_t)blockIdx.x * 32 + c;
+    const int64_t column = (int64_t)group_of() * 32 + c;
     float s = 0;
     if (column < columns) {
         int p = g;
@@ -405,7 +405,9 @@ int grad_groups(int64_t rows, int width)
 
 hipError_t launch_column_sums(const float *part, float *out, float *more, int64_t split, int parts, int64_t stride, int64_t columns, hipStream_t s)
 {
-    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((columns + 31) / 32)), dim3(1024), 0, s, part, out, more, split, parts, stride, columns);
+    dim3 grid;
+    if (!spread((columns + 31) / 32, 1024, grid)) return kNotTaken;
+    hipLaunchKernelGGL(column_sums_kernel, grid, dim3(1024), 0, s, part, out, more, split, parts, stride, columns);
     return hipGetLastError();
 }
 
@@ -421,10 +423,10 @@ hipError_t launch_norm_add(int dtype, const void *r, const void *x, const float 
         using E = std::remove_pointer_t<decltype(e)>;
         return by_width(width, [&](auto nt, auto nv) {
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-            const int64_t grid = (rows + kThreads / NT - 1) / (kThreads / NT);
-            if (grid > 0x7fffffff) return kNotTaken;
+            dim3 grid;
+            if (!spread((rows + kThreads / NT - 1) / (kThreads / NT), kThreads, grid)) return kNotTaken;
             auto *k = full ? norm_add_kernel<E, NT, NV, true> : norm_add_kernel<E, NT, NV, false>;
-            hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(kThreads), 0, s, (const E *)r, (const E *)x, gain, w, (E *)h, (E *)n, a);
+            hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, s, (const E *)r, (const E *)x, gain, w, (E *)h, (E *)n, a);
             return hipGetLastError();
         });
     });
@@ -460,10 +462,10 @@ hipError_t launch_norm_gate(int dtype, const void *x, const void *z, const float
         using E = std::remove_pointer_t<decltype(e)>;
         return by_width(width, [&](auto nt, auto nv) {
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-            const int64_t grid = (a.rows + kThreads / NT - 1) / (kThreads / NT);
-            if (grid > 0x7fffffff) return kNotTaken;
+            dim3 grid;
+            if (!spread((a.rows + kThreads / NT - 1) / (kThreads / NT), kThreads, grid)) return kNotTaken;
             auto *k = full ? norm_gate_kernel<E, NT, NV, true> : norm_gate_kernel<E, NT, NV, false>;
-            hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(kThreads), 0, s, (const E *)x, (const E *)z, w, (E *)y, a);
+            hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, s, (const E *)x, (const E *)z, w, (E *)y, a);
             return hipGetLastError();
         });
     });

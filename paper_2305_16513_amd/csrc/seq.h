@@ -96,6 +96,18 @@ inline bool sixteen(std::initializer_list<const void *> ps)
     return true;
 }
 
+// n workgroups of so many threads as a grid, `across` in y: a launch has fewer than 2^32 threads in x, so that more go on in z, the last of which may
+// reach beyond n.  False: more than 31 bits.
+inline bool spread(int64_t n, int threads, dim3 &grid, unsigned across = 1)
+{
+    const int64_t most = 0xffffffffll / threads, z = (n + most - 1) / most;
+    if (n > 0x7fffffff) return false;
+    grid = dim3((unsigned)(z > 1 ? (n + z - 1) / z : n), across, (unsigned)(z > 1 ? z : 1));
+    return true;
+}
+// Which of them this one is
+__device__ __forceinline__ unsigned group_of() { return blockIdx.z * gridDim.x + blockIdx.x; }
+
 // f with a null pointer of the storage type
 template <class F>
 hipError_t by_type(int dtype, F &&f)
