@@ -427,7 +427,7 @@ sws_status sws_conv2d_grad_weight_ws(const float *x, const float *gy, float *gw,
 
 /* The norm before a block, joined with the residual stream: per row
  *   h = r + gain * x,   n = h / sqrt(mean(h^2) + eps) * w
- * x may be NULL (h = r: then h is usually NULL too and is not written), gain may be NULL (ones).
+ * x may be NULL (h = r), gain may be NULL (ones), and so may h (it is not written then).
  *   r, x, h, n : rows * width elements, dense     gain, w : width floats
  * Errors: INVALID_ARG for an unknown dtype, negative rows, width < 1, gain without x, NULL r / w / n; UNSUPPORTED for width > 16384. */
 sws_status sws_norm_add(sws_dtype dtype, const void *r, const void *x, const float *gain, const float *w, void *h, void *n,

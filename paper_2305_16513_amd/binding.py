@@ -731,7 +731,8 @@ def _bytes_of(name, *sizes):
 
 
 def sws_norm_add(r, w, x=None, gain=None, eps=1e-6, h=None, n=None, stream=None):
-    """r, x [..., width], w, gain [width] fp32 -> (h, n): h = r + gain * x, n = h / sqrt(mean(h^2) + eps) * w.  Without x, h is r itself."""
+    """r, x [..., width], w, gain [width] fp32 -> (h, n): h = r + gain * x, n = h / sqrt(mean(h^2) + eps) * w.  Without x, h is r itself, or, where a tensor for it
+    is given, a copy there."""
     if h is None and n is None and stream is None and _calls is not None:
         got = _calls.norm_add(r, w, x, gain, eps)
         if got is not None:
@@ -742,11 +743,13 @@ def sws_norm_add(r, w, x=None, gain=None, eps=1e-6, h=None, n=None, stream=None)
     _params(gain, "gain", (width,), r)
     if x is not None:
         _rows(x, "x", r.shape, r, dense=True)
-        h = torch.empty_like(r) if h is None else _rows(h, "h", r.shape, r, dense=True)
+        h = torch.empty_like(r) if h is None else h
+    if h is not None:
+        _rows(h, "h", r.shape, r, dense=True)
     n = torch.empty_like(r) if n is None else _rows(n, "n", r.shape, r, dense=True)
-    _check(lib().sws_norm_add(_DTYPE[r.dtype], r.data_ptr(), _ptr(x), _ptr(gain), w.data_ptr(), _ptr(h) if x is not None else None, n.data_ptr(),
+    _check(lib().sws_norm_add(_DTYPE[r.dtype], r.data_ptr(), _ptr(x), _ptr(gain), w.data_ptr(), _ptr(h), n.data_ptr(),
                               r.numel() // width if width else 0, width, eps, _stream(stream)), "sws_norm_add")
-    return (r if x is None else h), n
+    return (r if h is None else h), n
 
 
 def sws_norm_add_grad(r, w, gn, x=None, gain=None, gh=None, eps=1e-6, gr=None, gx=None, stream=None):
