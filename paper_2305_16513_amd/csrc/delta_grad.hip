@@ -96,7 +96,8 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
         E *const qp = gq + b * sq.batch + t0 * sq.token + hk * sq.head, *const kp = gk + b * sk.batch + t0 * sk.token + hk * sk.head;
         for (int u = tid; u < rows * UNITS; u += kThreads) {
             const int r = u / UNITS, c0 = u % UNITS * PER, from = Keys::at(r, c0 / 4);
-            const v4u x = *(const v4u *)(outq + from), y = *(const v4u *)(outk + from);
+            const bool real = r < n;                  // (others are zeros, also where what they were multiplied with is not finite)
+            const v4u none = {0, 0, 0, 0}, x = real ? *(const v4u *)(outq + from) : none, y = real ? *(const v4u *)(outk + from) : none;
             if constexpr (FULL) {
                 *(v4u *)(qp + r * sq.token + c0) = x;
                 *(v4u *)(kp + r * sk.token + c0) = y;
@@ -104,8 +105,8 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
                 for (int e = 0; e < PER; ++e)
                     if (c0 + e < a.Dk) {
-                        qp[r * sq.token + c0 + e] = outq[from + e];
-                        kp[r * sk.token + c0 + e] = outk[from + e];
+                        qp[r * sq.token + c0 + e] = real ? outq[from + e] : (E)0.0f;
+                        kp[r * sk.token + c0 + e] = real ? outk[from + e] : (E)0.0f;
                     }
         }
     };
@@ -387,7 +388,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     for (int m = 0; m < 2; ++m) {
                         typename Vec<E>::v4 out;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) out[e] = (E)(bt * whole<E>(r1, 4 * m + e));
+                        for (int e = 0; e < 4; ++e) out[e] = mine < n ? (E)(bt * whole<E>(r1, 4 * m + e)) : (E)0.0f;
                         if constexpr (FULL) *(typename Vec<E>::v4 *)(gvp + d0 + 16 * m) = out;
                         else
 #pragma unroll

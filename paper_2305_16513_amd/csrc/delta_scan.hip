@@ -296,14 +296,14 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     old[1] = Mx<E>::mma(old[1], u0.p[n == 1], pf[1].p[n == 2]);
                     old[1] = Mx<E>::mma(old[1], u1.p[n == 1], pf[2].p[n == 2]);
                 }
-                const int64_t left = a.T - (int64_t)i * kChunk;
+                const int64_t left = a.T - (int64_t)i * kChunk, real = len - (int64_t)i * kChunk;
                 E *const oc = op + (int64_t)i * kChunk * a.o.token;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {         // (tokens that are not there have rows of zeros)
+                for (int t = 0; t < 2; ++t) {
                     typename Vec<E>::v4 out;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) out[e] = (E)(a.scale * old[t][e]);
                     const int token = 16 * tile[t] + l;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[e] = token < real ? (E)(a.scale * old[t][e]) : (E)0.0f;      // (a row of zeros times a state that is not finite is not zero)
                     if constexpr (FULL) {             // rows behind the last token lie behind the end of the buffer
                         const int st = (int)a.o.token * 2, many = left < kChunk ? (int)left : kChunk;
                         __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out), rsrc(oc, (unsigned)((many - 1) * st + 32)), token * st + 8 * gr, 0, 0);

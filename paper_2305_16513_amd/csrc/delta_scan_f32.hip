@@ -136,11 +136,11 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
                     y = mma<E>(y, u0, tri_frag(P, lower_at(t, 0)));
                     if (t >= 2) y = mma<E>(y, u1, tri_frag(P, lower_at(t, 1)));
                     const int64_t token = t0 + 16 * t + l;
-                    if (token < a.T && there > 0) {   // (tokens that are not there have rows of zeros)
+                    if (token < a.T && there > 0) {
                         E *p = op + token * a.o.token;
                         typename Vec<E>::v4 out;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) out[e] = (E)(a.scale * y[e]);
+                        for (int e = 0; e < 4; ++e) out[e] = token < len ? (E)(a.scale * y[e]) : (E)0.0f;   // (a row of zeros times a state that is not finite is not zero)
                         if constexpr (FULL) *(typename Vec<E>::v4 *)p = out;
                         else
 #pragma unroll
