@@ -48,16 +48,17 @@ __device__ __forceinline__ float gate(float g) { return g < kLowest ? kLowest : 
 // have the same.  This one is what two accumulator tiles hold (row 4 g + e of column lane % 16 each): a product becomes the
 // next one's operand in its registers.
 //
-// 16-bit storage: elements of q, k, v, go enter as they are.  What has been computed (states, U, N, T, P ...) enters as two pieces of the
-// storage type, hi + lo, whose sum is off by 2^-17 (bf16) or 2^-22 (fp16): rounded to one piece, each would cost as much as the rounding of the
-// output, and the state's errors would add up over the chunks.  The product of the two lower pieces is left out.  fp32: one piece, on the fp32
-// matrix instruction.
+// 16-bit storage: elements of q, k, v, go enter as they are.  What has been computed (states, U, N, T, P ...) is fp32 and enters a product as pieces of the
+// storage type: three in bf16, which together are the number; two in fp16, whose sum is off by 2^-22 of it, or 2^-25 where that is more.  So the fp32 outputs (states,
+// gradients of gates) are as exact as fp32 products would leave them, and do not depend on whether a call's tokens are few or many; one piece
+// would cost as much as the rounding of a 16-bit output, and the state's errors would add up over the chunks.  Products of pieces below the last piece's size
+// are left out.  fp32: one piece, on the fp32 matrix instruction.
 constexpr int kChunk = 64;
 
 template <class E> struct Mx;
 template <> struct Mx<__bf16> {
     typedef v8bf Frag;
-    static constexpr int NP = 2;
+    static constexpr int NP = 3;
     static __device__ __forceinline__ v4f mma(v4f c, Frag a, Frag b) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mx<_Float16> {
@@ -77,24 +78,29 @@ template <> struct Mx<float> {
 };
 template <class E> using Frag = typename Mx<E>::Frag;
 
-// Two numbers as their pieces of 16 bits, each pair a register.  An fp16 operand that is itself a product has to be one number for both its pieces: the
+// Two numbers as their pieces of 16 bits, the larger first, each pair a register.  An fp16 operand that is itself a product has to be one number for both its pieces: the
 // compiler would take the upper one from an instruction that rounds the exact product to 16 bits, and subtract it from the product
 // rounded to 32 bits first; next to a tie they are not the same.
 template <class E>
-__device__ __forceinline__ void pieces_of(float f, float g, unsigned &hi, unsigned &lo)
+__device__ __forceinline__ void pieces_of(float f, float g, unsigned (&p)[Mx<E>::NP])
 {
     if constexpr (std::is_same_v<E, _Float16>) {
         typedef _Float16 v2h __attribute__((ext_vector_type(2)));
         asm("" : "+v"(f));
         asm("" : "+v"(g));
         const v2h h = {(_Float16)f, (_Float16)g};
-        hi = __builtin_bit_cast(unsigned, h);
-        lo = __builtin_bit_cast(unsigned, v2h{(_Float16)(f - (float)h[0]), (_Float16)(g - (float)h[1])});
+        p[0] = __builtin_bit_cast(unsigned, h);
+        p[1] = __builtin_bit_cast(unsigned, v2h{(_Float16)(f - (float)h[0]), (_Float16)(g - (float)h[1])});
     } else {
+        // The first piece rounds to nearest, so that what is left has 16 bits at most and a sign of its own; the others cut these in two halves.
         typedef __bf16 v2b __attribute__((ext_vector_type(2)));
-        hi = __builtin_bit_cast(unsigned, __builtin_convertvector((v2f{f, g}), v2b));
-        asm("" : "+v"(hi));                           // (converted once, as a pair)
-        lo = __builtin_bit_cast(unsigned, __builtin_convertvector((v2f{f - __uint_as_float(hi << 16), g - __uint_as_float(hi & 0xffff0000u)}), v2b));
+        p[0] = __builtin_bit_cast(unsigned, __builtin_convertvector((v2f{f, g}), v2b));
+        asm("" : "+v"(p[0]));                         // (converted once, as a pair)
+        f -= __uint_as_float(p[0] << 16);
+        g -= __uint_as_float(p[0] & 0xffff0000u);
+        auto upper = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u); };
+        p[1] = upper(f, g);
+        p[2] = upper(f - __uint_as_float(__float_as_uint(f) & 0xffff0000u), g - __uint_as_float(__float_as_uint(g) & 0xffff0000u));
     }
 }
 
@@ -109,17 +115,18 @@ __device__ __forceinline__ Pieces<E> split(v4f a, v4f b)
     Pieces<E> r;
     if constexpr (Mx<E>::NP == 1) r.p[0] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     else {
-        v4u hi, lo;
+        constexpr int NP = Mx<E>::NP;
+        v4u u[NP];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            unsigned x, y;
-            pieces_of<E>(a[2 * e], a[2 * e + 1], x, y);
-            hi[e] = x, lo[e] = y;
-            pieces_of<E>(b[2 * e], b[2 * e + 1], x, y);
-            hi[2 + e] = x, lo[2 + e] = y;
+            unsigned x[NP], y[NP];
+            pieces_of<E>(a[2 * e], a[2 * e + 1], x);
+            pieces_of<E>(b[2 * e], b[2 * e + 1], y);
+#pragma unroll
+            for (int n = 0; n < NP; ++n) u[n][e] = x[n], u[n][2 + e] = y[n];
         }
-        r.p[0] = __builtin_bit_cast(Frag<E>, hi);
-        r.p[1] = __builtin_bit_cast(Frag<E>, lo);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) r.p[n] = __builtin_bit_cast(Frag<E>, u[n]);
     }
     return r;
 }
@@ -128,23 +135,25 @@ __device__ __forceinline__ Pieces<E> split(v4f a, v4f b)
 template <class E>
 __device__ __forceinline__ v4f mma(v4f c, const Frag<E> &a, const Pieces<E> &b)
 {
-    if constexpr (Mx<E>::NP == 2) c = Mx<E>::mma(c, a, b.p[1]);
-    return Mx<E>::mma(c, a, b.p[0]);
+#pragma unroll
+    for (int n = Mx<E>::NP - 1; n >= 0; --n) c = Mx<E>::mma(c, a, b.p[n]);
+    return c;
 }
 template <class E>
 __device__ __forceinline__ v4f mma(v4f c, const Pieces<E> &a, const Frag<E> &b)
 {
-    if constexpr (Mx<E>::NP == 2) c = Mx<E>::mma(c, a.p[1], b);
-    return Mx<E>::mma(c, a.p[0], b);
+#pragma unroll
+    for (int n = Mx<E>::NP - 1; n >= 0; --n) c = Mx<E>::mma(c, a.p[n], b);
+    return c;
 }
 template <class E>
 __device__ __forceinline__ v4f mma(v4f c, const Pieces<E> &a, const Pieces<E> &b)
 {
-    if constexpr (Mx<E>::NP == 2) {
-        c = Mx<E>::mma(c, a.p[0], b.p[1]);
-        c = Mx<E>::mma(c, a.p[1], b.p[0]);
-    }
-    return Mx<E>::mma(c, a.p[0], b.p[0]);
+#pragma unroll
+    for (int n = Mx<E>::NP - 1; n >= 0; --n)
+#pragma unroll
+        for (int i = 0; i <= n; ++i) c = Mx<E>::mma(c, a.p[i], b.p[n - i]);
+    return c;
 }
 
 // Rows of W elements in LDS, and operands out of them.  Four elements of a row, a quad, stand together.
@@ -311,41 +320,55 @@ __device__ __forceinline__ Pieces<E> get_pieces(const E *from, int at, int tid =
     return p;
 }
 
-// What the passes from chunk to chunk leave for the gradients, per chunk and 16 columns of the state: S (or the gradient of the state behind
+// What the passes from chunk to chunk leave for the gradients, in fp32, per chunk and 16 columns of the state: S (or the gradient of the state behind
 // the chunk) as DK / 32 operands whose contraction index is the key's element, U (or dR) as two whose contraction index is the token; every operand
-// as two units of 16 bytes a lane, the two pieces or (fp32) the two halves.  The gradients copy these into LDS as they are and need the operands whose contraction
-// index is the column of the state.
+// as two units of 16 bytes a lane.  The gradients lay these down in LDS in pieces, UNITS units of 16 bytes a lane (fp32: as they are), and need the operands whose
+// contraction index is the column of the state.
 template <class E> struct Kept {
-    static constexpr int64_t state(int DK) { return (int64_t)DK / 32 * 2048; }    // bytes
+    static constexpr int UNITS = Mx<E>::NP == 1 ? 2 : Mx<E>::NP, OPERAND = 1024 * UNITS;      // bytes of one in LDS
+    static constexpr int64_t state(int DK) { return (int64_t)DK / 32 * 2048; }    // bytes in memory
     static constexpr int64_t rows() { return 2 * 2048; }
     static __device__ __forceinline__ int place(int g, int r) { return (16 * g + (r ^ 4 * g)) * 16; }
 
-    static __device__ __forceinline__ void put(char *to, int kb, const Pieces<E> &p)
+    static __device__ __forceinline__ void put(char *to, int kb, v4f a, v4f b)
     {
-        v4u u[2];
-        if constexpr (Mx<E>::NP == 2) u[0] = __builtin_bit_cast(v4u, p.p[0]), u[1] = __builtin_bit_cast(v4u, p.p[1]);
-        else {
-            u[0] = __builtin_bit_cast(v4u, __builtin_shufflevector(p.p[0], p.p[0], 0, 1, 2, 3));
-            u[1] = __builtin_bit_cast(v4u, __builtin_shufflevector(p.p[0], p.p[0], 4, 5, 6, 7));
-        }
         char *const q = to + 2048 * kb + place(threadIdx.x % kWave / 16, threadIdx.x % 16);
-        *(v4u *)q = u[0];
-        *(v4u *)(q + 1024) = u[1];
+        *(v4f *)q = a;
+        *(v4f *)(q + 1024) = b;
+    }
+    // A lane's two units of an operand, lanes in the order of the units, from memory (`from` is the wavefront's); and to LDS
+    static __device__ __forceinline__ void load(const char *from, int lane, v4f (&u)[2])
+    {
+        const __amdgpu_buffer_rsrc_t b = rsrc(from, 2048);
+        u[0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane, 0, 0));
+        u[1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane + 1024, 0, 0));
+    }
+    static __device__ __forceinline__ void lay(char *to, int at, int lane, const v4f (&u)[2])
+    {
+        char *const q = to + OPERAND * at + 16 * lane;
+        if constexpr (Mx<E>::NP == 1) {
+            *(v4f *)q = u[0];
+            *(v4f *)(q + 1024) = u[1];
+        } else {
+            const Pieces<E> p = split<E>(u[0], u[1]);
+#pragma unroll
+            for (int n = 0; n < UNITS; ++n) *(Frag<E> *)(q + 1024 * n) = p.p[n];
+        }
     }
     // Of two groups of 16 columns in LDS, `group` bytes apart: lane's element (of the key, or token) is 16 j + lane % 16, the contraction index is the column.
     static __device__ __forceinline__ Pieces<E> columns(const char *p, int group, int j, int tid = threadIdx.x)
     {
         const int l = tid % 16, g = tid % kWave / 16;
         Pieces<E> r;
-        if constexpr (Mx<E>::NP == 2) {
-            const char *const q = p + place(l % 4, 4 * g + l / 4) + 2048 * (j >> 1) + 8 * (j & 1);
+        if constexpr (Mx<E>::NP > 1) {
+            const char *const q = p + place(l % 4, 4 * g + l / 4) + OPERAND * (j >> 1) + 8 * (j & 1);
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+            for (int n = 0; n < UNITS; ++n) {
                 const auto a = Tile<E, 32>::transposed((const E *)(q + 1024 * n)), b = Tile<E, 32>::transposed((const E *)(q + group + 1024 * n));
                 r.p[n] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
             }
         } else {
-            const char *const q = p + 2048 * (j >> 1) + 1024 * (j & 1) + 4 * (l % 4);
+            const char *const q = p + OPERAND * (j >> 1) + 1024 * (j & 1) + 4 * (l % 4);
 #pragma unroll
             for (int e = 0; e < 8; ++e) r.p[0][e] = *(const float *)(q + (e < 4 ? 0 : group) + place(l / 4, 4 * g + (e & 3)));
         }
@@ -355,11 +378,11 @@ template <class E> struct Kept {
     // other one first.
     static __device__ __forceinline__ void both(const char *p, int group, int m, Pieces<E> (&r)[2], int tid = threadIdx.x)
     {
-        if constexpr (Mx<E>::NP == 2) {
+        if constexpr (Mx<E>::NP > 1) {
             const int l = tid % 16, g = tid % kWave / 16, odd = 8 * (g & 1);
-            const char *const q = p + place(l % 4, 4 * g + l / 4) + 2048 * m;
+            const char *const q = p + place(l % 4, 4 * g + l / 4) + OPERAND * m;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+            for (int n = 0; n < UNITS; ++n) {
                 typename Vec<E>::v4 x[2][2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {

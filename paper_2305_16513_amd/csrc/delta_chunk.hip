@@ -19,7 +19,7 @@ namespace {
 
 int64_t tri_size(int dtype)
 {
-    return dtype == SWS_DTYPE_F32 ? tri_bytes<float>() : tri_bytes<__bf16>();
+    return dtype == SWS_DTYPE_F32 ? tri_bytes<float>() : dtype == SWS_DTYPE_BF16 ? tri_bytes<__bf16>() : tri_bytes<_Float16>();
 }
 
 // Few tokens: one after the other reads and writes the state once and needs no chunk, but takes as much time for every token, and a chunk takes as long

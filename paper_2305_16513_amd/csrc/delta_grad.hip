@@ -36,8 +36,9 @@ struct GradWs {
 template <class E>
 __device__ __forceinline__ float whole(const Pieces<E> &x, int e)
 {
-    float f = (float)x.p[0][e];
-    if constexpr (Mx<E>::NP == 2) f += (float)x.p[1][e];
+    float f = 0;
+#pragma unroll
+    for (int n = Mx<E>::NP - 1; n >= 0; --n) f += (float)x.p[n][e];
     return f;
 }
 
@@ -50,21 +51,20 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
     constexpr int NP = Mx<E>::NP, KB = DK / 32, KH = DK / 32;    // a wavefront's tiles of 16 of the keys' elements
     typedef Tile<E, DK> Keys;                         // of 64 tokens
     typedef Tile<E, 32> Values;                       // of 64 tokens, 32 of their values' elements
-    constexpr int SG = (int)Kept<E>::state(DK), UG = (int)Kept<E>::rows();       // bytes of 16 columns
-    struct Block {                                    // of 32 columns of the state S, dS, U, dR as they are kept, dO and V
+    constexpr int SG = KB * Kept<E>::OPERAND, UG = 2 * Kept<E>::OPERAND;         // bytes of 16 columns in LDS
+    struct Block {                                    // of 32 columns of the state S, dS, U, dR as operands, dO and V
         char s[2 * SG], d[2 * SG], u[2 * UG], r[2 * UG];
         E o[Values::size(kChunk)], v[Values::size(kChunk)];
     };
-    constexpr int NB = sizeof(E) == 4 && DK == 128 ? 1 : 2;      // (fp32: one, two would not fit)
     // After the columns dP and M as operands, then dq and dk; in the place of K and Q what dk has of dP and dS
-    constexpr int BYTES = NB * (int)sizeof(Block), AFTER = 8 * 3 * kWave * (int)sizeof(Pieces<E>), OUT = 2 * (int)sizeof(E) * Keys::size(kChunk);
+    constexpr int BYTES = (int)sizeof(Block), AFTER = 8 * 3 * kWave * (int)sizeof(Pieces<E>), OUT = 2 * (int)sizeof(E) * Keys::size(kChunk);
     constexpr int MOST = BYTES > AFTER ? (BYTES > OUT ? BYTES : OUT) : (AFTER > OUT ? AFTER : OUT);
     __shared__ __align__(16) char lds[MOST];
     __shared__ __align__(16) E keys[2][Keys::size(kChunk)];
     static_assert(sizeof(float) * kChunk * DK <= sizeof keys, "");
     __shared__ double sums[kChunk];
     __shared__ float betas[kChunk], dbs[kChunk], dots[2][2][kChunk], xdots[2][2][kChunk], parts[8];
-    Block *const blocks = (Block *)lds;
+    Block &m4 = *(Block *)lds;
     E *const ks = keys[0], *const qs = keys[1], *const outq = (E *)lds, *const outk = outq + Keys::size(kChunk);
     E *const operands = (E *)lds;
     v4f *const ex = (v4f *)keys;
@@ -113,9 +113,14 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 
     for (int hs = 0; hs < (MANY ? share : 1); ++hs) {
         const int h = hk * share + hs;
-        if constexpr (MANY) asm volatile("" : "+v"(tid));    // (not known to be the same for every head: addresses are not kept in registers over them)
-        const int lane = tid % kWave, l = tid % 16, gr = lane / 16, mine = 16 * w + l;      // token of the wavefront's own tile
-        const Keys ak(tid);
+        int lane, l, gr, mine;                        // mine: token of the wavefront's own tile
+        Keys ak(tid);
+        auto whereabouts = [&]() {                    // not known to be what they were before: addresses are not kept in registers until they are needed
+            asm volatile("" : "+v"(tid));
+            lane = tid % kWave, l = tid % 16, gr = lane / 16, mine = 16 * w + l;
+            ak = Keys(tid);
+        };
+        whereabouts();
         const Values av(tid);
         const int64_t at = ((b * a.Hv + h) * ws.chunks + c);
         G *const ggp = gg + (b * a.T + t0) * a.Hv + h, *const gbp = gbeta + (b * a.T + t0) * a.Hv + h;
@@ -125,65 +130,67 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             continue;
         }
         const int64_t kept = at * (ws.cols / 16);
-        const char *const up = (const char *)ws.u + kept * UG, *const rp = (const char *)ws.r + kept * UG;
-        const char *const sp = (const char *)ws.s + kept * SG, *const dp = (const char *)ws.ds + kept * SG;
+        const char *const up = (const char *)ws.u + kept * Kept<E>::rows(), *const rp = (const char *)ws.r + kept * Kept<E>::rows();
+        const char *const sp = (const char *)ws.s + kept * Kept<E>::state(DK), *const dp = (const char *)ws.ds + kept * Kept<E>::state(DK);
         const E *const op = go + b * a.o.batch + t0 * a.o.token + h * a.o.head, *const vp = v + b * a.v.batch + t0 * a.v.token + h * a.v.head;
         float inner = 0;                              // <S, dS>
-        // The next 32 columns are on their way to the other block during the products of these: what is kept goes there by itself, a kilobyte an instruction;
-        // eight threads a row of dO and V.
+        // The next 32 columns are on their way to registers during the products of these.  S and dS have 64 KB lanes' shares of operands, U and dR 256 together: a thread
+        // takes one of S, the same of dS and one of U or dR; with KB = 2 half of the threads S and dS, the others U and dR.  Eight threads a row of dO and V.
         typedef typename Vec<E>::v4 V4;
         V4 ov, vv;
-        auto copy = [&](const char *from, char *to, int bytes) {
-            typedef __attribute__((address_space(1))) const void *Global;
-            typedef __attribute__((address_space(3))) void *Local;
-            for (int i = wave; i < bytes / 1024; i += 8)
-                __builtin_amdgcn_global_load_lds((Global)(from + 1024 * i + 16 * lane), (Local)(to + 1024 * i), 16, 0, 0);
-        };
+        v4f s4[2], d4[2], u4[2];
+        const bool low = wave < 4;
         auto fetch = [&](int d0) {
-            Block &to = blocks[d0 / 32 % NB];
-            copy(sp + (int64_t)d0 / 16 * SG, to.s, 2 * SG);
-            copy(dp + (int64_t)d0 / 16 * SG, to.d, 2 * SG);
-            copy(up + (int64_t)d0 / 16 * UG, to.u, 2 * UG);
-            copy(rp + (int64_t)d0 / 16 * UG, to.r, 2 * UG);
+            const int64_t so = (int64_t)d0 / 16 * Kept<E>::state(DK), uo = (int64_t)d0 / 16 * Kept<E>::rows();
+            if constexpr (KB == 4) {
+                Kept<E>::load(sp + so + 2048 * wave, lane, s4);
+                Kept<E>::load(dp + so + 2048 * wave, lane, d4);
+                Kept<E>::load((low ? up : rp) + uo + 2048 * w, lane, u4);
+            } else {
+                Kept<E>::load((low ? sp + so : up + uo) + 2048 * w, lane, s4);
+                Kept<E>::load((low ? dp + so : rp + uo) + 2048 * w, lane, d4);
+            }
             const int r = tid / 8, c4 = 4 * (tid % 8);
-            ov = vv = V4{};
-            if (r < n) {
-                const E *po = op + r * a.o.token + d0 + c4, *pv = vp + r * a.v.token + d0 + c4;
-                if constexpr (FULL) {
-                    ov = *(const V4 *)po;
-                    vv = *(const V4 *)pv;
-                } else
+            if constexpr (FULL) {                     // rows that are not there lie behind the end of a buffer
+                constexpr int SIZE = (int)sizeof(E);
+                auto row = [&](const E *from, const Steps &s) {
+                    const __amdgpu_buffer_rsrc_t b = rsrc(from + d0, (unsigned)((n - 1) * (int)s.token * SIZE + 32 * SIZE));
+                    const int off = r < n ? r * (int)s.token * SIZE + c4 * SIZE : 0x7ffffff0;
+                    if constexpr (SIZE == 4) return __builtin_bit_cast(V4, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0));
+                    else return __builtin_bit_cast(V4, __builtin_amdgcn_raw_buffer_load_b64(b, off, 0, 0));
+                };
+                ov = row(op, a.o);
+                vv = row(vp, a.v);
+            } else {
+                ov = vv = V4{};
+                if (r < n) {
+                    const E *po = op + r * a.o.token + d0 + c4, *pv = vp + r * a.v.token + d0 + c4;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (e < a.Dv - d0 - c4) {
                             ov[e] = po[e];
                             vv[e] = pv[e];
                         }
+                }
             }
         };
-        auto stage = [&](int d0) -> const Block & {
-            Block &here = blocks[d0 / 32 % NB];
-            if (NB == 1 && d0 > 0) {
-                __syncthreads();
-                fetch(d0);
+        auto stage = [&](int d0) {
+            __syncthreads();                          // the last columns have been read
+            if constexpr (KB == 4) {
+                Kept<E>::lay(m4.s, wave, lane, s4);
+                Kept<E>::lay(m4.d, wave, lane, d4);
+                Kept<E>::lay(low ? m4.u : m4.r, w, lane, u4);
+            } else {
+                Kept<E>::lay(low ? m4.s : m4.u, w, lane, s4);
+                Kept<E>::lay(low ? m4.d : m4.r, w, lane, d4);
             }
-            *(V4 *)(here.o + Values::at(tid / 8, tid % 8)) = ov;
-            *(V4 *)(here.v + Values::at(tid / 8, tid % 8)) = vv;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the copies too
+            *(V4 *)(m4.o + Values::at(tid / 8, tid % 8)) = ov;
+            *(V4 *)(m4.v + Values::at(tid / 8, tid % 8)) = vv;
+            if (KB == 4 || low)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) inner += s4[0][e] * d4[0][e] + s4[1][e] * d4[1][e];
             __syncthreads();
-            if (NB == 2 && d0 + 32 < ws.cols) fetch(d0 + 32);    // (everybody is done with that block: the barrier)
-            for (int i = wave; i < 2 * SG / 2048; i += 8) {
-                const v4u s0 = *(const v4u *)(here.s + 2048 * i + 16 * lane), s1 = *(const v4u *)(here.s + 2048 * i + 1024 + 16 * lane);
-                const v4u e0 = *(const v4u *)(here.d + 2048 * i + 16 * lane), e1 = *(const v4u *)(here.d + 2048 * i + 1024 + 16 * lane);
-                if constexpr (NP == 2) {
-                    const Pieces<E> x = {__builtin_bit_cast(Frag<E>, s0), __builtin_bit_cast(Frag<E>, s1)}, y = {__builtin_bit_cast(Frag<E>, e0), __builtin_bit_cast(Frag<E>, e1)};
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) inner += whole<E>(x, e) * whole<E>(y, e);
-                } else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) inner += __uint_as_float(s0[e]) * __uint_as_float(e0[e]) + __uint_as_float(s1[e]) * __uint_as_float(e1[e]);
-            }
-            return here;
+            if (d0 + 32 < ws.cols) fetch(d0 + 32);
         };
         // The five blocks of dP or M that the wavefront's own tile of tokens is in: x[t], t <= w, rows are tokens j of tile t, columns tokens i of its own;
         // x[t + 1], t >= w, rows are tokens i of tile t, columns tokens j of its own.  (Slots, not tiles: which ones there are depends on
@@ -264,24 +271,27 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             v4f x1[2][KH], x3[2][KH];                 // dO S^T, U dS^T
 #pragma unroll
             for (int i = 0; i < KH; ++i) x1[0][i] = x1[1][i] = x3[0][i] = x3[1][i] = zero;
+#pragma unroll 1
             for (int d0 = 0; d0 < ws.cols; d0 += 32) {
-                const Block &m4 = stage(d0);
+                stage(d0);
                 const Frag<E> om[2] = {av.rows(m4.o, 2 * th, 0), av.rows(m4.o, 2 * th + 1, 0)};
                 Pieces<E> um[2];
                 Kept<E>::both(m4.u, UG, th, um, tid);
 #pragma unroll
                 for (int i = 0; i < KH / 2; ++i) {
-                    Pieces<E> st[2], dt[2];
+                    Pieces<E> st[2];
                     Kept<E>::both(m4.s, SG, KH / 2 * dh + i, st, tid);
-                    Kept<E>::both(m4.d, SG, KH / 2 * dh + i, dt, tid);
 #pragma unroll
                     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            x1[tt][2 * i + m] = mma<E>(x1[tt][2 * i + m], om[tt], st[m]);
-                            x3[tt][2 * i + m] = mma<E>(x3[tt][2 * i + m], um[tt], dt[m]);
-                        }
+                        for (int m = 0; m < 2; ++m) x1[tt][2 * i + m] = mma<E>(x1[tt][2 * i + m], om[tt], st[m]);
                     __builtin_amdgcn_sched_barrier(0);    // (or all the reads go out first, into more registers than there are)
+                    Kept<E>::both(m4.d, SG, KH / 2 * dh + i, st, tid);
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) x3[tt][2 * i + m] = mma<E>(x3[tt][2 * i + m], um[tt], st[m]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 const Frag<E> o1 = dh ? om[1] : om[0];
                 const Pieces<E> u1 = dh ? um[1] : um[0];
@@ -302,6 +312,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     for (int m = NP - 1; m >= 0; --m) x[t] = Mx<E>::mma(x[t], l4.p[m], r4.p[m]);
                 }
             }
+            whereabouts();
             inner = sum_lanes(inner, kWave);
             if (lane == 0) parts[wave] = inner;
             leave([&](int, int, float y, int, int) { return a.scale * y; });
@@ -365,8 +376,9 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
             for (int i = 0; i < KH; ++i) x2[0][i] = x2[1][i] = zero;
             E *const gvp = gv + b * sv.batch + t0 * sv.token + h * sv.head + mine * sv.token + 4 * gr;
+#pragma unroll 1
             for (int d0 = 0; d0 < ws.cols; d0 += 32) {
-                const Block &m4 = stage(d0);
+                stage(d0);
                 Pieces<E> rm[2], um;
                 Kept<E>::both(m4.r, UG, th, rm, tid);
 #pragma unroll
@@ -402,6 +414,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     x[t] = mma<E>(x[t], l4, r4);
                 }
             }
+            whereabouts();
             inner = sum_lanes(inner, kWave);
             if (lane == 0) parts[wave] = inner;
             float db = 0;                             // of token `mine`, the part of this lane's rows

@@ -26,14 +26,13 @@ namespace {
 // Wavefronts: of the states, of the terms beside them (not where only states are wanted), two that load K and V (dO), two that load T, the factors and Q
 constexpr int scan_threads(int NS, int MODE) { return kWave * ((MODE == KEEP ? 2 * NS : 4 * NS) + 4); }
 
-// The workgroup's LDS: two of K, Q, V (or dO) and the chunk's factors, T (or T^T); two of what goes from the wavefronts of the states to those
-// beside them, or back: forward the operands of S, and U; backward the accumulators of scale Q^T (exp(G) dO) and of scale P^T dO; the halves of K S.
+// The workgroup's LDS: two of K, Q, V (or dO) and the chunk's factors, T (or T^T); what goes from the wavefronts of the states to those
+// beside them, or back: forward the operands of S, and two of U; backward two of scale Q^T (exp(G) dO) and of scale P^T dO, as accumulators; the halves of K S.
 template <class E, int DK, int NS, int MODE>
 struct ScanLds {
-    static constexpr int XS = DK / 32 * 2 * kWave * 8, XU = 2 * 2 * kWave * 8;
+    static constexpr int XS = MODE == FORWARD ? DK / 32 * Mx<E>::NP * kWave : DK / 16 * kWave, XU = 4 * kWave;
     static constexpr bool QUERIES = MODE != KEEP;
-    static_assert(XS * 2 == DK / 16 * kWave * 16 && XU * 2 == 4 * kWave * 16, "");
-    E xs[QUERIES ? 2 : 1][QUERIES ? NS * XS : 8], xu[QUERIES ? 2 : 1][QUERIES ? NS * XU : 8];
+    v4f xs[MODE == BACKWARD ? 2 : 1][QUERIES ? NS * XS : 1], xu[QUERIES ? 2 : 1][QUERIES ? NS * XU : 1];
     v4f half[2][NS][4 * kWave];
     E ks[2][kChunk * DK], qs[QUERIES ? 2 : 1][QUERIES ? kChunk * DK : 8];
     v4u ts[tri_bytes<E>() / 16];
@@ -41,17 +40,23 @@ struct ScanLds {
     float fs[2][4 * kChunk];                          // (three of 64; the last is nobody's)
 };
 
-// x[t] += M_t0 a + M_t1 b over the blocks of a triangular matrix that are there, whose operands are at(t, block); the products of one accumulator four apart
-template <class E, class F>
-__device__ __forceinline__ void tri_mul(v4f (&x)[4], const Pieces<E> (&m)[kFrags], const Pieces<E> &a, const Pieces<E> &b, F &&at)
+// Where the operand of tile row t and block kb of a triangular matrix is, -1: there is none.  Of its blocks one has four operands, the other two.
+template <bool UPPER> __device__ __forceinline__ constexpr int tri_at(int t, int kb)
+{
+    return UPPER ? (kb >= t / 2 ? upper_at(t, kb) : -1) : kb <= t / 2 ? lower_at(t, kb) : -1;
+}
+
+// x[t] += M_t,kb a over one block of a triangular matrix; the products of one accumulator as far apart as there are tiles
+template <class E, bool UPPER>
+__device__ __forceinline__ void tri_mul(v4f (&x)[4], const Pieces<E> (&m)[kFrags], const Pieces<E> &a, int kb)
 {
 #pragma unroll
-    for (int n = 2; n >= 0; --n)                      // lower times upper, upper times lower, upper times upper
+    for (int n = Mx<E>::NP - 1; n >= 0; --n)          // the lesser products first
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int i = 0; i <= n; ++i)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (at(t, kb) >= 0) x[t] = Mx<E>::mma(x[t], m[at(t, kb)].p[n == 2], (kb ? b : a).p[n == 1]);
+                if (tri_at<UPPER>(t, kb) >= 0) x[t] = Mx<E>::mma(x[t], m[tri_at<UPPER>(t, kb)].p[i], a.p[n - i]);
 }
 
 // (Wavefronts per SIMD: the compiler sees no LDS; below half of the registers accumulators are ordinary ones and need no moves.)
@@ -60,7 +65,7 @@ __global__ __launch_bounds__(scan_threads(NS, MODE)) __attribute__((amdgpu_waves
 void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E *__restrict__ v, E *__restrict__ o, float *__restrict__ state,
                        ScanWs ws, DeltaArgs a)
 {
-    constexpr int NL = 128, W = 16 * NS, TRI = tri_bytes<E>(), KB = DK / 32, KT = DK / 16, HB = KB / 2, HT = KT / 2;
+    constexpr int NL = 128, NP = Mx<E>::NP, W = 16 * NS, TRI = tri_bytes<E>(), KB = DK / 32, KT = DK / 16, HB = KB / 2, HT = KT / 2;
     constexpr int KINDS = MODE == FORWARD ? 2 : 3, T_AT = MODE == BACKWARD ? 1 : 0, P_AT = MODE == BACKWARD ? 2 : 1;
     typedef ScanLds<E, DK, NS, MODE> Lds;
     typedef Tile<E, DK> Keys;
@@ -110,20 +115,27 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 
     if (wave < 2 * NS) {
         float *const sp = state && (len > 0 || MODE == BACKWARD) ? state + (slot * a.Hv + h) * (int64_t)a.Dk * a.Dv : nullptr;
-        const int my = col0 + 16 * w + l;             // this lane's column
         v4f s[HT];
+        auto each = [&](auto &&f) {                   // f(element, its place in the state) of this lane's that are there
+            int t = threadIdx.x;
+            asm volatile("" : "+v"(t));               // (the places are not kept in registers until the end)
+            const int my = col0 + 16 * w + t % 16;    // this lane's column
 #pragma unroll
-        for (int i = 0; i < HT; ++i)
+            for (int i = 0; i < HT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 16 * (HT * hf + i) + 4 * gr + e;
-                s[i][e] = sp && r < a.Dk && my < a.Dv ? sp[(int64_t)r * a.Dv + my] : 0.0f;
-            }
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 16 * (HT * hf + i) + 4 * (t % kWave / 16) + e;
+                    if (r < a.Dk && my < a.Dv) f(i, e, r * a.Dv + my);
+                }
+        };
+#pragma unroll
+        for (int i = 0; i < HT; ++i) s[i] = zero;
+        if (sp) each([&](int i, int e, int at) { s[i][e] = sp[at]; });
         Pieces<E> sx[HB];
 #pragma unroll
         for (int kb = 0; kb < HB; ++kb) {
             sx[kb] = split<E>(s[2 * kb], s[2 * kb + 1]);
-            if constexpr (MODE == FORWARD) put_pieces<E>(xs[0] + w * XS, HB * hf + kb, sx[kb]);
+            if constexpr (MODE == FORWARD) put_pieces<E>((E *)(xs[0] + w * XS), HB * hf + kb, sx[kb]);
         }
         barrier();
         if constexpr (MODE == BACKWARD) barrier();
@@ -136,7 +148,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             if constexpr (MODE != FORWARD) {
                 char *const to = (char *)ws.s + kept * Kept<E>::state(DK);
 #pragma unroll
-                for (int kb = 0; kb < HB; ++kb) Kept<E>::put(to, HB * hf + kb, sx[kb]);
+                for (int kb = 0; kb < HB; ++kb) Kept<E>::put(to, HB * hf + kb, s[2 * kb], s[2 * kb + 1]);
             }
             auto factor = [&](int which, int t) { return *(const v4f *)(fc + which * kChunk + 16 * t + 4 * gr); };
             // Everything that is read of K for one product goes out in one go, and is taken as it comes: a read takes as long as eight products.
@@ -153,7 +165,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
             for (int kb = 0; kb < HB; ++kb)
 #pragma unroll
-                for (int n = 1; n >= 0; --n)
+                for (int n = NP - 1; n >= 0; --n)
 #pragma unroll
                     for (int t = 0; t < 4; ++t) x[t] = Mx<E>::mma(x[t], kf[kb][t], sx[kb].p[n]);
 #pragma unroll
@@ -167,8 +179,14 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             Frag<E> cf[HT][2];
 #pragma unroll
             for (int t = 0; t < 4; ++t) f1[t] = m.half[hf ^ 1][w][t * kWave + lane];
+            // (T's larger block; the other one when K S, V and the factors have been used)
+            constexpr bool UPPER = MODE == BACKWARD;
+            auto tri_read = [&](int kb) {
 #pragma unroll
-            for (int f = 0; f < kFrags; ++f) tf[f] = get_pieces<E>((const E *)m.ts, f);
+                for (int t = 0; t < 4; ++t)
+                    if (tri_at<UPPER>(t, kb) >= 0) tf[tri_at<UPPER>(t, kb)] = get_pieces<E>((const E *)m.ts, tri_at<UPPER>(t, kb));
+            };
+            tri_read(UPPER);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -182,28 +200,29 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     const v4f v4 = widen(vt[t]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[t][e] = v4[e] - f0[t][e] * x[t][e];
-                    f1[t] = factor(1, t);
                 }
                 const Pieces<E> n0 = split<E>(x[0], x[1]), n1 = split<E>(x[2], x[3]);
+                tri_read(1);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) x[t] = zero;
-                tri_mul(x, tf, n0, n1, [](int t, int kb) { return kb <= t / 2 ? lower_at(t, kb) : -1; });
+                tri_mul<E, false>(x, tf, n0, 0);
+                tri_mul<E, false>(x, tf, n1, 1);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) f1[t] = factor(1, t);
 #pragma unroll
                 for (int j = 0; j < HT; ++j) {
                     cf[j][0] = cols(kc, 0, j);
                     cf[j][1] = cols(kc, 1, j);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (MODE == KEEP) {
-                    if (hf) Kept<E>::put(up, 1, split<E>(x[2], x[3]));
-                    else Kept<E>::put(up, 0, split<E>(x[0], x[1]));
-                } else {
-                    v4f *const to = (v4f *)(xu[p] + w * XU) + 2 * hf * kWave + lane;
+                if constexpr (MODE == KEEP) Kept<E>::put(up, hf, hf ? x[2] : x[0], hf ? x[3] : x[1]);
+                else {
+                    v4f *const to = xu[p] + w * XU + 2 * hf * kWave + lane;
                     to[0] = hf ? x[2] : x[0];
                     to[kWave] = hf ? x[3] : x[1];
                 }
             } else {
-                const v4f *const zc = (const v4f *)(xu[p] + w * XU) + lane;
+                const v4f *const zc = xu[p] + w * XU + lane;
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {         // dU
                     const v4f z = zc[t * kWave];
@@ -214,24 +233,25 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     for (int e = 0; e < 4; ++e) f1[t][e] = -gm[e] * bt[e];
                 }
                 const Pieces<E> u0 = split<E>(x[0], x[1]), u1 = split<E>(x[2], x[3]);
+                tri_read(0);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) x[t] = zero;
-                tri_mul(x, tf, u0, u1, [](int t, int kb) { return kb >= t / 2 ? upper_at(t, kb) : -1; });
+                tri_mul<E, true>(x, tf, u1, 1);
+                tri_mul<E, true>(x, tf, u0, 0);
 #pragma unroll
                 for (int j = 0; j < HT; ++j) {
                     cf[j][0] = cols(kc, 0, j);
                     cf[j][1] = cols(kc, 1, j);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (hf) Kept<E>::put(up, 1, split<E>(x[2], x[3]));
-                else Kept<E>::put(up, 0, split<E>(x[0], x[1]));
+                Kept<E>::put(up, hf, hf ? x[2] : x[0], hf ? x[3] : x[1]);
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[t][e] *= f1[t][e];
             d0 = split<E>(x[0], x[1]), d1 = split<E>(x[2], x[3]);
-            const v4f *const yc = (const v4f *)(xs[QUERIES ? p : 0] + w * XS) + HT * hf * kWave + lane;
+            const v4f *const yc = xs[QUERIES ? p : 0] + w * XS + HT * hf * kWave + lane;
 #pragma unroll
             for (int j = 0; j < HT; ++j) {
                 if constexpr (MODE == BACKWARD) {
@@ -243,7 +263,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     for (int e = 0; e < 4; ++e) s[j][e] *= all;
             }
 #pragma unroll
-            for (int n = 1; n >= 0; --n) {
+            for (int n = NP - 1; n >= 0; --n) {
 #pragma unroll
                 for (int j = 0; j < HT; ++j) s[j] = Mx<E>::mma(s[j], cf[j][0], d0.p[n]);
 #pragma unroll
@@ -252,18 +272,11 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
             for (int kb = 0; kb < HB; ++kb) {
                 sx[kb] = split<E>(s[2 * kb], s[2 * kb + 1]);
-                if constexpr (MODE == FORWARD) put_pieces<E>(xs[p ^ 1] + w * XS, HB * hf + kb, sx[kb]);
+                if constexpr (MODE == FORWARD) put_pieces<E>((E *)(xs[0] + w * XS), HB * hf + kb, sx[kb]);      // (the last ones have been read)
             }
             barrier();
         }
-        if (MODE != KEEP && sp && my < a.Dv)
-#pragma unroll
-            for (int i = 0; i < HT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 16 * (HT * hf + i) + 4 * gr + e;
-                    if (r < a.Dk) sp[(int64_t)r * a.Dv + my] = s[i][e];
-                }
+        if (MODE != KEEP && sp) each([&](int i, int e, int at) { sp[at] = s[i][e]; });
         return;
     }
 
@@ -288,14 +301,16 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             const int there = a.Dv - (col0 + 16 * w + 4 * gr);
             v4f y[2], old[2];
             auto finish = [&](int i) {                // O of chunk i, of which `old` is exp(G) Q S
-                const v4f *const uc = (const v4f *)(xu[i & 1] + w * XU) + lane;
+                const v4f *const uc = xu[i & 1] + w * XU + lane;
                 const Pieces<E> u0 = split<E>(uc[0], uc[kWave]), u1 = split<E>(uc[2 * kWave], uc[3 * kWave]);
 #pragma unroll
-                for (int n = 2; n >= 0; --n) {
-                    old[0] = Mx<E>::mma(old[0], u0.p[n == 1], pf[0].p[n == 2]);
-                    old[1] = Mx<E>::mma(old[1], u0.p[n == 1], pf[1].p[n == 2]);
-                    old[1] = Mx<E>::mma(old[1], u1.p[n == 1], pf[2].p[n == 2]);
-                }
+                for (int n = NP - 1; n >= 0; --n)
+#pragma unroll
+                    for (int m = 0; m <= n; ++m) {
+                        old[0] = Mx<E>::mma(old[0], u0.p[n - m], pf[0].p[m]);
+                        old[1] = Mx<E>::mma(old[1], u0.p[n - m], pf[1].p[m]);
+                        old[1] = Mx<E>::mma(old[1], u1.p[n - m], pf[2].p[m]);
+                    }
                 const int64_t left = a.T - (int64_t)i * kChunk, real = len - (int64_t)i * kChunk;
                 E *const oc = op + (int64_t)i * kChunk * a.o.token;
 #pragma unroll
@@ -318,7 +333,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             barrier();
             for (int i = 0; i < chunks; ++i) {
                 const int p = i & 1;
-                const E *const sc = xs[p] + w * XS, *const qc = qs[p];
+                const E *const sc = (const E *)(xs[0] + w * XS), *const qc = qs[p];
                 Frag<E> qf[KB][2];
                 Pieces<E> sf[KB];
                 float gm[2];
@@ -337,7 +352,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                    for (int n = 1; n >= 0; --n)
+                    for (int n = NP - 1; n >= 0; --n)
 #pragma unroll
                         for (int t = 0; t < 2; ++t) y[t] = Mx<E>::mma(y[t], sf[kb].p[n], qf[kb][t]);
                 if (i > 0) finish(i - 1);
@@ -355,7 +370,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                 const int p = i & 1;
                 const E *const vc = vs[p], *const qc = qs[p];
                 const float *const gp = ws.factors + (head * ws.chunks + first + i * step) * (int64_t)(3 * kChunk);
-                v4f *const zc = (v4f *)(xu[p] + w * XU) + lane, *const yc = (v4f *)(xs[p] + w * XS) + HT * hf * kWave + lane;
+                v4f *const zc = xu[p] + w * XU + lane, *const yc = xs[p] + w * XS + HT * hf * kWave + lane;
                 v4f g4[4], y[4], z[2];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) g4[t] = *(const v4f *)(gp + 16 * t + 4 * gr);
@@ -369,7 +384,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                 __builtin_amdgcn_sched_barrier(0);
                 z[0] = z[1] = zero;
 #pragma unroll
-                for (int n = 1; n >= 0; --n) {
+                for (int n = NP - 1; n >= 0; --n) {
                     z[0] = Mx<E>::mma(z[0], pf[0].p[n], o0);
                     z[1] = Mx<E>::mma(z[1], pf[2].p[n], o1);
                     z[0] = Mx<E>::mma(z[0], pf[1].p[n], o1);
@@ -389,7 +404,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
                 for (int j = 0; j < HT; ++j) r[j] = zero;
 #pragma unroll
-                for (int n = 1; n >= 0; --n) {
+                for (int n = NP - 1; n >= 0; --n) {
 #pragma unroll
                     for (int j = 0; j < HT; ++j) r[j] = Mx<E>::mma(r[j], cf[j][0], y0.p[n]);
 #pragma unroll

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) {
             sx[kb] = split<E>(s[2 * kb], s[2 * kb + 1]);
-            if constexpr (MODE != FORWARD) Kept<E>::put((char *)ws.s + kept * Kept<E>::state(DK), kb, sx[kb]);
+            if constexpr (MODE != FORWARD) Kept<E>::put((char *)ws.s + kept * Kept<E>::state(DK), kb, s[2 * kb], s[2 * kb + 1]);
         }
 
         auto factor = [&](int which, int t) { return *(const v4f *)(fs + which * kChunk + 16 * t + 4 * gr); };
@@ -119,8 +119,8 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
                 if (t >= 2) x[t] = mma<E>(x[t], tri_frag(T, lower_at(t, 1)), n1);
             }
             if constexpr (MODE == KEEP) {
-                Kept<E>::put(up, 0, split<E>(x[0], x[1]));
-                Kept<E>::put(up, 1, split<E>(x[2], x[3]));
+                Kept<E>::put(up, 0, x[0], x[1]);
+                Kept<E>::put(up, 1, x[2], x[3]);
             } else {
                 const Pieces<E> u0 = split<E>(x[0], x[1]), u1 = split<E>(x[2], x[3]);
                 E *const op = o + b * a.o.batch + h * a.o.head + col0 + 16 * w + 4 * gr;
@@ -185,8 +185,8 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
                 if (t < 2) x[t] = mma<E>(x[t], tri_frag(T, upper_at(t, 0)), u0);
                 x[t] = mma<E>(x[t], tri_frag(T, upper_at(t, 1)), u1);
             }
-            Kept<E>::put(up, 0, split<E>(x[0], x[1]));
-            Kept<E>::put(up, 1, split<E>(x[2], x[3]));
+            Kept<E>::put(up, 0, x[0], x[1]);
+            Kept<E>::put(up, 1, x[2], x[3]);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const v4f gm = factor(0, t), bt = factor(2, t);
