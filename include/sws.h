@@ -495,7 +495,10 @@ typedef struct {
  *   S_t = exp(g_t) S_{t-1} + k_t u_t^T,   u_t = beta_t (v_t - exp(g_t) S_{t-1}^T k_t),   o_t = scale * S_t^T q_t
  * g <= 0 (0 keeps all, -inf forgets all).  S_0 is the sequence's place in `state` (pool * Hv * Dk * Dv floats, dense), which is
  * replaced by the last S, or zero where state is NULL.  A few tokens are taken one after the other, more in chunks of 64 on the
- * matrix cores: within a chunk the corrections solve a triangular system.  fp16 storage: states and corrections stay below 65504.
+ * matrix cores: within a chunk the corrections solve a triangular system.  fp32 numbers (states, gradients of fp32 gates) are as exact as
+ * fp32 products leave them, whatever the storage and the number of tokens.  fp16 storage, in chunks: an S or u is held to 2^-22 of itself
+ * or 2^-27 of the largest of v and S_0, whichever is more, and stays below 256 times that largest one; products q.k stay below 65504;
+ * backward the same of go and the last S's gradient.
  *   q, k : B T Hk Dk     v, o : B T Hv Dv     g, beta : B T Hv
  * Errors: INVALID_ARG for NULL pointers, unknown dtypes, sizes below 1 (B, T: 0 is allowed), Hv no multiple of Hk, negative
  * distances, slots without state, neither slots nor a place for every sequence, too little workspace; UNSUPPORTED for Dk > 128, Dv > 256. */

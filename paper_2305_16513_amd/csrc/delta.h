@@ -49,7 +49,7 @@ __device__ __forceinline__ float gate(float g) { return g < kLowest ? kLowest : 
 // next one's operand in its registers.
 //
 // 16-bit storage: elements of q, k, v, go enter as they are.  What has been computed (states, U, N, T, P ...) is fp32 and enters a product as pieces of the
-// storage type: three in bf16, which together are the number; two in fp16, whose sum is off by 2^-22 of it, or 2^-25 where that is more.  So the fp32 outputs (states,
+// storage type: three in bf16, which together are the number; two in fp16, whose sum is off by 2^-22 of it, or 2^-25 where that is more (see scale_of).  So the fp32 outputs (states,
 // gradients of gates) are as exact as fp32 products would leave them, and do not depend on whether a call's tokens are few or many; one piece
 // would cost as much as the rounding of a 16-bit output, and the state's errors would add up over the chunks.  Products of pieces below the last piece's size
 // are left out.  fp32: one piece, on the fp32 matrix instruction.
@@ -402,6 +402,53 @@ template <class E> struct Kept {
     }
 };
 
+// fp16 numbers reach from 2^-24 to 65504; states and corrections are as large as the values that they are made of.  They are linear in the values and the state before the
+// first token, and backward in the gradients of the outputs and of the last state.  So a value head's passes work on these times a power of two and take it back
+// in what they give.  It brings the largest of them to 4 .. 8 if it is below (else a loss that is a mean over tokens would leave its gradients where the
+// pieces have few bits), to 128 .. 256 if it is beyond (a state may then grow 256-fold), and is 1 between: bits that are worth 2^-25 are worth that of numbers of that size.
+// Numbers that are not finite do not count.
+template <class E> constexpr bool kScaled = std::is_same_v<E, _Float16>;
+
+// The power of two for a largest magnitude, given as its fp32 bits
+__device__ __forceinline__ float scale_of(unsigned top)
+{
+    const int at = (int)(top >> 23) - 127, by = at < 2 ? 2 - at : at < 8 ? 0 : 7 - at, e = by < -100 ? -100 : by > 100 ? 100 : by;
+    return top ? __uint_as_float((unsigned)(127 + e) << 23) : 1.0f;
+}
+
+// A magnitude's bits, 0 where it is not finite
+__device__ __forceinline__ unsigned magnitude(float f)
+{
+    const unsigned u = __float_as_uint(f) & 0x7fffffffu;
+    return u < 0x7f800000u ? u : 0u;
+}
+
+__device__ __forceinline__ unsigned max_lanes(unsigned v)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const unsigned t = (unsigned)__shfl_xor((int)v, d);
+        v = v > t ? v : t;
+    }
+    return v;
+}
+
+// The largest magnitudes of each chunk, two numbers a chunk (of the values, and with the first chunk the state; of the outputs' gradients, and the last state's); of which
+// a wavefront makes the scale of all of a sequence's
+__device__ __forceinline__ float scale_over(const unsigned *tops, int chunks, int which)
+{
+    unsigned top = 0;
+    for (int c = threadIdx.x % kWave; c < chunks; c += kWave) top = top > tops[2 * c + which] ? top : tops[2 * c + which];
+    return scale_of((unsigned)__builtin_amdgcn_readfirstlane((int)max_lanes(top)));
+}
+
+// What the first pass needs for that (go, gstate: gradients only)
+struct Magnitudes {
+    const void *v, *go;
+    const float *state, *gstate;
+    unsigned *tops;
+};
+
 // The passes from chunk to chunk: outputs; states and U for the gradients; the backward pass
 enum ScanMode { FORWARD, KEEP, BACKWARD };
 
@@ -409,6 +456,8 @@ struct ScanWs {
     const char *tri;                                  // per chunk T beta and P, or T beta, T^T and P^T
     const float *factors;
     void *u, *s;                                      // KEEP: U and the states before the chunks; BACKWARD: dR and the gradients of those behind
+    const unsigned *tops;                             // fp16: magnitudes per chunk
+    float *scales;                                    // fp16: per value head the scale of U and S, and that of dR and dS, for the gradients
     int chunks, cols;                                 // of a sequence; of the state as it is kept (a multiple of 32)
 };
 

@@ -5,15 +5,15 @@ namespace sws {
 
 hipError_t launch_delta_step(int dtype, int gate_dtype, const void *q, const void *k, const void *v, const void *g, const void *beta, void *o,
                              float *pool, const DeltaArgs &a, hipStream_t s);
-hipError_t launch_delta_prep(int dtype, int gate_dtype, const void *q, const void *k, const void *g, const void *beta, char *tri, float *factors, int chunks,
-                             bool full, bool grad, const DeltaArgs &a, hipStream_t s);
+hipError_t launch_delta_prep(int dtype, int gate_dtype, const void *q, const void *k, const void *g, const void *beta, char *tri, float *factors,
+                             const Magnitudes &mg, int chunks, bool full, bool grad, const DeltaArgs &a, hipStream_t s);
 hipError_t launch_delta_scan_16(int dtype, int mode, const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws,
                                 const DeltaArgs &a, hipStream_t s);
 hipError_t launch_delta_scan_f32(int mode, const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws, const DeltaArgs &a,
                                  hipStream_t s);
 hipError_t launch_delta_grad(int dtype, int gate_dtype, const void *q, const void *k, const void *v, const void *g, const void *beta, const void *go, void *gq,
-                             void *gk, void *gv, void *gg, void *gbeta, const void *u, const void *r, const void *st, const void *ds, int chunks, int cols,
-                             bool full, const DeltaArgs &a, const Steps (&gs)[3], hipStream_t s);
+                             void *gk, void *gv, void *gg, void *gbeta, const void *u, const void *r, const void *st, const void *ds, const float *scales,
+                             int chunks, int cols, bool full, const DeltaArgs &a, const Steps (&gs)[3], hipStream_t s);
 
 namespace {
 
@@ -21,6 +21,8 @@ int64_t tri_size(int dtype)
 {
     return dtype == SWS_DTYPE_F32 ? tri_bytes<float>() : dtype == SWS_DTYPE_BF16 ? tri_bytes<__bf16>() : tri_bytes<_Float16>();
 }
+
+int64_t tops_size(int dtype) { return dtype == SWS_DTYPE_F16 ? 8 : 0; }
 
 // Few tokens: one after the other reads and writes the state once and needs no chunk, but takes as much time for every token, and a chunk takes as long
 // with one token as with 64.  How many are few depends on what a token costs: with few states a chain of LDS and barriers, with many the
@@ -64,14 +66,14 @@ int columns(const DeltaArgs &a) { return (a.Dv + 31) / 32 * 32; }
 int64_t delta_rule_bytes(int dtype, const DeltaArgs &a)
 {
     if (few(a)) return 0;
-    return a.B * a.Hv * ((a.T + kChunk - 1) / kChunk) * (2 * tri_size(dtype) + kFactorBytes);
+    return a.B * a.Hv * ((a.T + kChunk - 1) / kChunk) * (2 * tri_size(dtype) + kFactorBytes + tops_size(dtype));
 }
 
-// T, T^T and P^T; the chunks' factors; U and dR; the states before the chunks and the gradients of those behind them
+// T, T^T and P^T; the chunks' factors; U and dR; the states before the chunks and the gradients of those behind them; magnitudes and the heads' scales
 int64_t delta_rule_grad_bytes(int dtype, const DeltaArgs &a)
 {
     const int64_t n = a.B * a.Hv * ((a.T + kChunk - 1) / kChunk);
-    return n * (3 * tri_size(dtype) + kFactorBytes + 8 * (int64_t)(kChunk + keys(a)) * columns(a));
+    return n * (3 * tri_size(dtype) + kFactorBytes + 8 * (int64_t)(kChunk + keys(a)) * columns(a) + tops_size(dtype)) + a.B * a.Hv * tops_size(dtype);
 }
 
 hipError_t launch_delta_rule(int dtype, int gate_dtype, const void *q, const void *k, const void *v, const void *g, const void *beta, void *o,
@@ -81,9 +83,12 @@ hipError_t launch_delta_rule(int dtype, int gate_dtype, const void *q, const voi
     const int64_t chunks = (a.T + kChunk - 1) / kChunk;
     if (chunks > 0x7fffff) return kNotTaken;
     char *tri = (char *)ws.p;
-    float *factors = (float *)(tri + a.B * a.Hv * chunks * 2 * tri_size(dtype));
-    hipError_t e = launch_delta_prep(dtype, gate_dtype, q, k, g, beta, tri, factors, (int)chunks, full_keys(dtype, a, q, k), false, a, s);
-    if (e == hipSuccess) e = launch_scan(dtype, FORWARD, q, k, v, o, pool, {tri, factors, nullptr, nullptr, (int)chunks, 0}, a, s);
+    const int64_t n = a.B * a.Hv * chunks;
+    float *factors = (float *)(tri + n * 2 * tri_size(dtype));
+    unsigned *tops = (unsigned *)((char *)factors + n * kFactorBytes);
+    hipError_t e = launch_delta_prep(dtype, gate_dtype, q, k, g, beta, tri, factors, {v, nullptr, pool, nullptr, tops}, (int)chunks, full_keys(dtype, a, q, k), false,
+                                     a, s);
+    if (e == hipSuccess) e = launch_scan(dtype, FORWARD, q, k, v, o, pool, {tri, factors, nullptr, nullptr, tops, nullptr, (int)chunks, 0}, a, s);
     return e;
 }
 
@@ -97,13 +102,15 @@ hipError_t launch_delta_rule_grad(int dtype, int gate_dtype, const void *q, cons
     char *tri = (char *)ws.p;
     float *factors = (float *)(tri + n * 3 * tri_size(dtype));
     float *u = factors + n * (kFactorBytes / 4), *r = u + n * kChunk * cols, *st = r + n * kChunk * cols, *ds = st + n * keys(a) * cols;
+    unsigned *tops = (unsigned *)(ds + n * keys(a) * cols);
+    float *scales = (float *)(tops + 2 * n);
     const bool fk = full_keys(dtype, a, q, k);
-    hipError_t e = launch_delta_prep(dtype, gate_dtype, q, k, g, beta, tri, factors, nc, fk, true, a, s);
-    if (e == hipSuccess) e = launch_scan(dtype, KEEP, q, k, v, nullptr, const_cast<float *>(state), {tri, factors, u, st, nc, cols}, a, s);
-    if (e == hipSuccess) e = launch_scan(dtype, BACKWARD, q, k, v, const_cast<void *>(go), gstate, {tri, factors, r, ds, nc, cols}, a, s);
+    hipError_t e = launch_delta_prep(dtype, gate_dtype, q, k, g, beta, tri, factors, {v, go, state, gstate, tops}, nc, fk, true, a, s);
+    if (e == hipSuccess) e = launch_scan(dtype, KEEP, q, k, v, nullptr, const_cast<float *>(state), {tri, factors, u, st, tops, scales, nc, cols}, a, s);
+    if (e == hipSuccess) e = launch_scan(dtype, BACKWARD, q, k, v, const_cast<void *>(go), gstate, {tri, factors, r, ds, tops, scales, nc, cols}, a, s);
     const bool full = fk && full_grads(dtype, a, v, go, gq, gk, gv, gs);
     if (e == hipSuccess)
-        e = launch_delta_grad(dtype, gate_dtype, q, k, v, g, beta, go, gq, gk, gv, gg, gbeta, u, r, st, ds, nc, cols, full, a, gs, s);
+        e = launch_delta_grad(dtype, gate_dtype, q, k, v, g, beta, go, gq, gk, gv, gg, gbeta, u, r, st, ds, scales, nc, cols, full, a, gs, s);
     return e;
 }
 

@@ -30,6 +30,7 @@ constexpr int kThreads = 512;
 
 struct GradWs {
     const void *u, *r, *s, *ds;                       // U, dR, S, dS as the passes before have left them (see Kept)
+    const float *scales;                              // fp16: of U and S, and of dR and dS
     int chunks, cols;
 };
 
@@ -129,6 +130,10 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             if (tid < rows) ggp[(int64_t)tid * a.Hv] = gbp[(int64_t)tid * a.Hv] = (G)0.0f;
             continue;
         }
+        // What is made of U or S and of dR or dS has both scales, and so has what dO is multiplied into, by way of `scale`
+        const float rise = kScaled<E> ? ws.scales[2 * (b * a.Hv + h)] : 1.0f, grise = kScaled<E> ? ws.scales[2 * (b * a.Hv + h) + 1] : 1.0f;
+        const float fall = 1.0f / rise, gfall = 1.0f / grise, scale = kScaled<E> ? a.scale * grise : a.scale;
+        auto whole_again = [&](float f) { return kScaled<E> ? f * fall * gfall : f; };
         const int64_t kept = at * (ws.cols / 16);
         const char *const up = (const char *)ws.u + kept * Kept<E>::rows(), *const rp = (const char *)ws.r + kept * Kept<E>::rows();
         const char *const sp = (const char *)ws.s + kept * Kept<E>::state(DK), *const dp = (const char *)ws.ds + kept * Kept<E>::state(DK);
@@ -315,7 +320,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             whereabouts();
             inner = sum_lanes(inner, kWave);
             if (lane == 0) parts[wave] = inner;
-            leave([&](int, int, float y, int, int) { return a.scale * y; });
+            leave([&](int, int, float y, int, int) { return scale * y; });
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
                 const Pieces<E> p0 = operand(tt, 0), p1 = operand(tt, 1), p3 = operand(tt, 2);
@@ -323,7 +328,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const double g1 = sums[16 * (2 * th + tt) + 4 * gr + e];
-                    ga[e] = a.scale * decay<E>((float)g1);
+                    ga[e] = scale * decay<E>((float)g1);
                     de[e] = decay<E>((float)(sums[kChunk - 1] - g1));
                 }
 #pragma unroll
@@ -355,6 +360,9 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
                 for (int i = 0; i < KH; ++i) {
                     ex[((w * 2 + tt) * KH + i) * kWave + lane] = x3[tt][i];
+                    if constexpr (kScaled<E>)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x1[tt][i][e] = whole_again(x1[tt][i][e]);
                     if constexpr (MANY) total[tt][i] += x1[tt][i];
                     else to_row(outq, tt, i, x1[tt][i]);
                 }
@@ -368,7 +376,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     const float t = __shfl_down(s, d);
                     if (lane + d < kWave) s += t;
                 }
-                if (lane < rows) ggp[(int64_t)lane * a.Hv] = (G)(lane < n ? s : 0.0f);
+                if (lane < rows) ggp[(int64_t)lane * a.Hv] = (G)(lane < n ? whole_again(s) : 0.0f);
             }
             __syncthreads();
         } else {
@@ -400,7 +408,7 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     for (int m = 0; m < 2; ++m) {
                         typename Vec<E>::v4 out;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) out[e] = mine < n ? (E)(bt * whole<E>(r1, 4 * m + e)) : (E)0.0f;
+                        for (int e = 0; e < 4; ++e) out[e] = mine < n ? (E)((kScaled<E> ? gfall * bt : bt) * whole<E>(r1, 4 * m + e)) : (E)0.0f;
                         if constexpr (FULL) *(typename Vec<E>::v4 *)(gvp + d0 + 16 * m) = out;
                         else
 #pragma unroll
@@ -468,13 +476,17 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (l == 4 * gr + e && mine < rows)
-                    gbp[(int64_t)mine * a.Hv] = (G)(mine < n ? vd[e] + dbs[mine] + (xdots[1][0][mine] + xdots[1][1][mine]) : 0.0f);
+                    gbp[(int64_t)mine * a.Hv] =
+                        (G)(mine < n ? whole_again((kScaled<E> ? rise * vd[e] : vd[e]) + dbs[mine] + (xdots[1][0][mine] + xdots[1][1][mine])) : 0.0f);
             __syncthreads();
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                 for (int i = 0; i < KH; ++i) {
-                    const v4f y = x2[tt][i] + ex[((w * 2 + tt) * KH + i) * kWave + lane];
+                    v4f y = x2[tt][i] + ex[((w * 2 + tt) * KH + i) * kWave + lane];
+                    if constexpr (kScaled<E>)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = whole_again(y[e]);
                     if constexpr (MANY) total[tt][i] += y;
                     else to_row(outk, tt, i, y);
                 }
@@ -494,12 +506,12 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 }  // namespace
 
 hipError_t launch_delta_grad(int dtype, int gate_dtype, const void *q, const void *k, const void *v, const void *g, const void *beta, const void *go, void *gq,
-                             void *gk, void *gv, void *gg, void *gbeta, const void *u, const void *r, const void *st, const void *ds, int chunks, int cols,
-                             bool full, const DeltaArgs &a, const Steps (&gs)[3], hipStream_t s)
+                             void *gk, void *gv, void *gg, void *gbeta, const void *u, const void *r, const void *st, const void *ds,
+                             const float *scales, int chunks, int cols, bool full, const DeltaArgs &a, const Steps (&gs)[3], hipStream_t s)
 {
     dim3 grid;
     if (!spread(a.B * a.Hk * chunks, kThreads, grid)) return kNotTaken;
-    const GradWs ws{u, r, st, ds, chunks, cols};
+    const GradWs ws{u, r, st, ds, scales, chunks, cols};
     return by_type(dtype, [&](auto *t) {
         using E = std::remove_pointer_t<decltype(t)>;
         auto with = [&](auto *x) {

@@ -3,7 +3,7 @@
 //   T = (I + A)^-1,  A_ij = beta_i D_ij k_i.k_j (j < i),      P_ij = D_ij q_i.k_j (j <= i)
 //
 // T with its columns scaled by beta, and P (or, for the gradients, that, T^T and P^T) go to the workspace as operands in the order in which lanes take them, with the chunk's factors
-// exp(G), exp(G_63 - G) and beta.
+// exp(G), exp(G_63 - G) and beta; in fp16 also the largest magnitudes of the chunk's values (and of their outputs' gradients), which the passes behind are scaled by.
 //
 // A workgroup takes one chunk of one value head.  Wavefront w multiplies tile row w of K K^T and Q K^T.  T in fp32: each
 // wavefront inverts one 16 x 16 block of the diagonal, a lane a column, by substitution; blocks are then joined twice,
@@ -44,7 +44,7 @@ __device__ __forceinline__ void block_put(float *to, v4f v, float sign)
 
 template <class E, class G, int DK, bool FULL, bool GRAD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) == 4 ? 2 : 4))) void delta_prep_kernel(const E *__restrict__ q, const E *__restrict__ k, const G *__restrict__ g,
-                                                         const G *__restrict__ beta, char *__restrict__ tri, float *__restrict__ factors, int chunks,
+                                                         const G *__restrict__ beta, char *__restrict__ tri, float *__restrict__ factors, Magnitudes mg, int chunks,
                                                          DeltaArgs a)
 {
     typedef Tile<E, DK> Keys;
@@ -56,6 +56,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
     const Keys at;
     __shared__ double sums[kChunk];
     __shared__ float betas[kChunk];
+    __shared__ unsigned tops[2][4];                   // of each wavefront
     const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int64_t head = group_of() / (unsigned)chunks, b = (unsigned)head / (unsigned)a.Hv;
     const int c = group_of() % (unsigned)chunks;
@@ -64,6 +65,48 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
     const int64_t t0 = (int64_t)c * kChunk, left = tokens_of(a, b) - t0;
     if (left <= 0) return;
     const int n = left < kChunk ? (int)left : kChunk;
+    if constexpr (kScaled<E>) {                       // (the barriers in between are those of the matrices)
+        unsigned top[2] = {0, 0};
+        auto look = [&](const E *p, int64_t step, unsigned &to) {
+            if (a.Dv % 8 == 0 && step % 8 == 0 && ((uintptr_t)p & 15) == 0) {      // eight elements a lane, whole rows a wavefront
+                const int units = a.Dv / 8, many = kWave / units, r0 = lane / units, d = 8 * (lane % units);
+                for (int r = w * many + r0; r < n && r0 < many; r += 4 * many) {
+                    float f[8];
+                    load8<true>(p + r * step + d, 8, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const unsigned u = magnitude(f[e]);
+                        to = to > u ? to : u;
+                    }
+                }
+            } else
+                for (int r = w; r < n; r += 4)
+                    for (int d = lane; d < a.Dv; d += kWave) {
+                        const unsigned u = magnitude((float)p[r * step + d]);
+                        to = to > u ? to : u;
+                    }
+        };
+        look((const E *)mg.v + b * a.v.batch + t0 * a.v.token + h * a.v.head, a.v.token, top[0]);
+        if constexpr (GRAD) look((const E *)mg.go + b * a.o.batch + t0 * a.o.token + h * a.o.head, a.o.token, top[1]);
+        if (c == 0) {
+            auto look_at_state = [&](const float *s, int64_t place, unsigned &to) {
+                const float *const p = s + (place * a.Hv + h) * (int64_t)a.Dk * a.Dv;
+                for (int i = threadIdx.x; i < a.Dk * a.Dv; i += 256) {
+                    const unsigned u = magnitude(p[i]);
+                    to = to > u ? to : u;
+                }
+            };
+            const int64_t place = a.slots ? a.slots[b] : b;
+            if (mg.state && (!a.slots || (place >= 0 && place < a.pool))) look_at_state(mg.state, place, top[0]);
+            if constexpr (GRAD)
+                if (mg.gstate) look_at_state(mg.gstate, b, top[1]);
+        }
+#pragma unroll
+        for (int i = 0; i < (GRAD ? 2 : 1); ++i) {
+            top[i] = max_lanes(top[i]);
+            if (lane == 0) tops[i][w] = top[i];
+        }
+    }
     {
         Rows<E, DK, 256, FULL> kr, qr;
         kr.load(k + b * a.k.batch + t0 * a.k.token + hk * a.k.head, a.k.token, n, a.Dk, threadIdx.x);
@@ -90,6 +133,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
         qr.store(qs, threadIdx.x);
     }
     __syncthreads();
+    if constexpr (kScaled<E>)
+        if (threadIdx.x < (GRAD ? 2 : 1)) {
+            const unsigned *t = tops[threadIdx.x], x = t[0] > t[1] ? t[0] : t[1], y = t[2] > t[3] ? t[2] : t[3];
+            mg.tops[2 * (head * chunks + c) + threadIdx.x] = x > y ? x : y;
+        }
     const int l = lane % 16, gr = lane / 16;
     v4f kk[4], qk[4];
 #pragma unroll
@@ -196,8 +244,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
 
 }  // namespace
 
-hipError_t launch_delta_prep(int dtype, int gate_dtype, const void *q, const void *k, const void *g, const void *beta, char *tri, float *factors, int chunks,
-                             bool full, bool grad, const DeltaArgs &a, hipStream_t s)
+hipError_t launch_delta_prep(int dtype, int gate_dtype, const void *q, const void *k, const void *g, const void *beta, char *tri, float *factors,
+                             const Magnitudes &mg, int chunks, bool full, bool grad, const DeltaArgs &a, hipStream_t s)
 {
     dim3 grid;
     if (!spread(a.B * a.Hv * chunks, 256, grid)) return kNotTaken;
@@ -206,8 +254,8 @@ hipError_t launch_delta_prep(int dtype, int gate_dtype, const void *q, const voi
         auto with = [&](auto *u) {
             using G = std::remove_pointer_t<decltype(u)>;
             auto go = [&](auto *kernel) {
-                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const E *)q, (const E *)k, (const G *)g, (const G *)beta, tri, factors, chunks,
-                                   a);
+                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const E *)q, (const E *)k, (const G *)g, (const G *)beta, tri, factors, mg,
+                                   chunks, a);
                 return hipGetLastError();
             };
             if (a.Dk <= 64) {

@@ -90,6 +90,8 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
     if (state && a.slots && (slot < 0 || slot >= a.pool)) len = 0;
     const int chunks = chunks_of(len);
     const int first = MODE == BACKWARD ? chunks - 1 : 0, step = MODE == BACKWARD ? -1 : 1;   // the i-th chunk is first + i * step
+    // (the last product's rounding is to the storage type, or fp32: the scale and its inverse are powers of two)
+    const float rise = kScaled<E> && wave < (MODE == KEEP ? 2 : 4) * NS ? scale_over(ws.tops + 2 * head * ws.chunks, chunks, MODE == BACKWARD) : 1.0f, fall = 1.0f / rise;
     auto barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
     auto tri_of = [&](int i, int kind) {
         return (const E *)(ws.tri + (head * ws.chunks + first + i * step) * (int64_t)(KINDS * TRI) + kind * TRI);
@@ -130,7 +132,8 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
         };
 #pragma unroll
         for (int i = 0; i < HT; ++i) s[i] = zero;
-        if (sp) each([&](int i, int e, int at) { s[i][e] = sp[at]; });
+        if (sp) each([&](int i, int e, int at) { s[i][e] = kScaled<E> ? rise * sp[at] : sp[at]; });
+        if (kScaled<E> && MODE != FORWARD && blockIdx.y == 0 && threadIdx.x == 0 && chunks > 0) ws.scales[2 * head + (MODE == BACKWARD)] = rise;
         Pieces<E> sx[HB];
 #pragma unroll
         for (int kb = 0; kb < HB; ++kb) {
@@ -199,7 +202,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                 for (int t = 0; t < 4; ++t) {         // N
                     const v4f v4 = widen(vt[t]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[t][e] = v4[e] - f0[t][e] * x[t][e];
+                    for (int e = 0; e < 4; ++e) x[t][e] = (kScaled<E> ? rise * v4[e] : v4[e]) - f0[t][e] * x[t][e];
                 }
                 const Pieces<E> n0 = split<E>(x[0], x[1]), n1 = split<E>(x[2], x[3]);
                 tri_read(1);
@@ -276,12 +279,13 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             }
             barrier();
         }
-        if (MODE != KEEP && sp) each([&](int i, int e, int at) { sp[at] = s[i][e]; });
+        if (MODE != KEEP && sp) each([&](int i, int e, int at) { sp[at] = kScaled<E> ? fall * s[i][e] : s[i][e]; });
         return;
     }
 
     if (MODE != KEEP && wave < 4 * NS) {              // beside the states: tokens of tiles hf and 3 - hf
         const int tile[2] = {hf, 3 - hf};
+        const float scale = !kScaled<E> ? a.scale : a.scale * (MODE == FORWARD ? fall : rise);
         Pieces<E> pf[3];                              // of P: one block of the first and two of the other; of P^T: two and one
         auto fetch = [&](int i) {
             const E *const t = tri_of(i, P_AT);
@@ -318,7 +322,7 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                     typename Vec<E>::v4 out;
                     const int token = 16 * tile[t] + l;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) out[e] = token < real ? (E)(a.scale * old[t][e]) : (E)0.0f;      // (a row of zeros times a state that is not finite is not zero)
+                    for (int e = 0; e < 4; ++e) out[e] = token < real ? (E)(scale * old[t][e]) : (E)0.0f;      // (a row of zeros times a state that is not finite is not zero)
                     if constexpr (FULL) {             // rows behind the last token lie behind the end of the buffer
                         const int st = (int)a.o.token * 2, many = left < kChunk ? (int)left : kChunk;
                         __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out), rsrc(oc, (unsigned)((many - 1) * st + 32)), token * st + 8 * gr, 0, 0);
@@ -392,11 +396,11 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
 #pragma unroll
                 for (int t = 0; t < 4; ++t)           // dO in accumulator layout is its operand
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[t][e] = a.scale * g4[t][e] * (float)(t < 2 ? o0 : o1)[4 * (t & 1) + e];
+                    for (int e = 0; e < 4; ++e) y[t][e] = scale * g4[t][e] * (float)(t < 2 ? o0 : o1)[4 * (t & 1) + e];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[t][e] *= a.scale;
+                    for (int e = 0; e < 4; ++e) z[t][e] *= scale;
                     zc[tile[t] * kWave] = z[t];
                 }
                 const Pieces<E> y0 = split<E>(y[0], y[1]), y1 = split<E>(y[2], y[3]);

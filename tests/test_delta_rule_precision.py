@@ -58,3 +58,21 @@ def test_a_state_does_not_depend_on_how_many_tokens_a_call_has(dtype):
     for t in range(0, 192, 8):
         B.sws_delta_rule(*[x[:, t:t + 8] for x in ins], 0.25, state=pieces)
     assert off(whole, pieces.double().cpu()) <= EXACT["state"]
+
+
+# Gradients of a loss that is a mean over tokens, small values and states, states beyond what fp16 holds (which single tokens take too); of these, little is forgotten: fp16's
+# pieces hold 2^-25 of the largest number, not of what is left of it
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("go_size,v_size,state_size", [(1e-4, 1, 0.3), (1e-6, 1, 0.3), (1, 1e-3, 1e-3), (1, 1, 1e5), (100, 3000, 1e6), (1e-5, 1e-4, 1e-7)])
+@pytest.mark.parametrize("hv,dk,dv", [(2, 128, 64), (1, 64, 128), (3, 40, 50)])
+def test_sizes_far_from_one(dtype, go_size, v_size, state_size, hv, dk, dv):
+    got, want = calls(torch.Generator().manual_seed(dk + dv), dtype, 2, 150, 1, hv, dk, dv, go_size, v_size, state_size, mild=state_size > 1)
+    for name, bound in EXACT.items():
+        assert off(got[name], want[name]) <= bound, (name, off(got[name], want[name]))
+    # outputs of 16 bits: their own rounding, of a fixed size below fp16's normal numbers
+    for name in ("o", "gq", "gk", "gv"):
+        x, r = got[name].double().cpu(), want[name].detach()
+        fits = r.abs() < 60000
+        allowed = U.HALF[got[name].dtype] * r.abs() * (1 + 2.0 ** -6) + 2e-5 * r.square().mean().sqrt() + (2.0 ** -25 if dtype == "f16" else 0)
+        assert bool(((x - r).abs() <= allowed)[fits].all()), name
