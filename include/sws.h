@@ -493,7 +493,8 @@ typedef struct {
 /* The gated delta rule: per sequence and value head (which reads queries and keys of head h / (Hv / Hk)) a state S of Dk x Dv
  * floats that every token decays, corrects and reads:
  *   S_t = exp(g_t) S_{t-1} + k_t u_t^T,   u_t = beta_t (v_t - exp(g_t) S_{t-1}^T k_t),   o_t = scale * S_t^T q_t
- * g <= 0 (0 keeps all, -inf forgets all).  S_0 is the sequence's place in `state` (pool * Hv * Dk * Dv floats, dense), which is
+ * g <= 0 (0 keeps all, -inf forgets all).  A k, v, g or beta that is not finite leaves the outputs in front of its token as they are,
+ * a v those of other columns; those behind it are not finite.  S_0 is the sequence's place in `state` (pool * Hv * Dk * Dv floats, dense), which is
  * replaced by the last S, or zero where state is NULL.  A few tokens are taken one after the other, more in chunks of 64 on the
  * matrix cores: within a chunk the corrections solve a triangular system.  fp32 numbers (states, gradients of fp32 gates) are as exact as
  * fp32 products leave them, whatever the storage and the number of tokens.  fp16 storage, in chunks: an S or u is held to 2^-22 of itself
@@ -507,7 +508,8 @@ sws_status sws_delta_rule(const sws_delta *d, const void *q, const void *k, cons
                           float *state, void *workspace, int64_t workspace_bytes, sws_stream_t stream);
 
 /* Its gradients, given go, that of o.  state: B Hv Dk Dv floats, the S_0 of the forward call as it was before, or NULL (zero).
- * gstate, or NULL: in, the gradient of the last S; out, that of S_0.  (No slots: place b is sequence b's.)
+ * gstate, or NULL: in, the gradient of the last S; out, that of S_0.  (No slots: place b is sequence b's.)  Gradients of a sequence with
+ * numbers that are not finite are not defined, other sequences' are as they are.
  *   gq, gk, gv : as q, k, v, at distances d->gq ...     gg, gbeta : B T Hv elements of gate_dtype, dense
  * Errors: as above. */
 int64_t sws_delta_rule_grad_workspace(const sws_delta *d);

@@ -43,6 +43,9 @@ __device__ __forceinline__ float gate(float g) { return g < kLowest ? kLowest : 
 // All exponents are of sums of gates <= 0, so nothing overflows however strong the decay.  Tokens that are not there have beta = 0, g = 0 and
 // rows of zeros: they change nothing.
 //
+// Where a number is not finite, zeros of T and P would carry it to earlier tokens.  Rows of T are then solved one by one, and forward products with T and P are done again
+// without the rows of N or U that are not finite, and those behind them.
+//
 // Every product is of 16 x 16 tiles with a contraction of 32.  An operand is eight elements a lane: of row (or column) lane % 16 the
 // contraction indices 4 g + e and 16 + 4 g + e (g = lane / 16, e = 0 .. 3) of a block of 32; the order of a contraction is free as long as both sides
 // have the same.  This one is what two accumulator tiles hold (row 4 g + e of column lane % 16 each): a product becomes the
@@ -103,6 +106,9 @@ __device__ __forceinline__ void pieces_of(float f, float g, unsigned (&p)[Mx<E>:
         p[2] = upper(f - __uint_as_float(__float_as_uint(f) & 0xffff0000u), g - __uint_as_float(__float_as_uint(g) & 0xffff0000u));
     }
 }
+
+// Numbers of this magnitude and more have no finite pieces (fp16: what rounds to infinity; bf16: rounding the largest fp32 numbers up would, too)
+template <class E> constexpr float kLimit = std::is_same_v<E, _Float16> ? 65520.0f : std::is_same_v<E, __bf16> ? 3.3895314e38f : __builtin_inff();
 
 // A computed operand
 template <class E> struct Pieces {

@@ -57,6 +57,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
     __shared__ double sums[kChunk];
     __shared__ float betas[kChunk];
     __shared__ unsigned tops[2][4];                   // of each wavefront
+    __shared__ int broken;                            // A has numbers that are not finite
     const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int64_t head = group_of() / (unsigned)chunks, b = (unsigned)head / (unsigned)a.Hv;
     const int c = group_of() % (unsigned)chunks;
@@ -111,6 +112,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
         Rows<E, DK, 256, FULL> kr, qr;
         kr.load(k + b * a.k.batch + t0 * a.k.token + hk * a.k.head, a.k.token, n, a.Dk, threadIdx.x);
         qr.load(q + b * a.q.batch + t0 * a.q.token + hk * a.q.head, a.q.token, n, a.Dk, threadIdx.x);
+        if (threadIdx.x == 0) broken = 0;
         if (w == 0) {
             const bool there = lane < n;
             const int64_t tk = t0 + lane;
@@ -164,11 +166,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
         for (int e = 0; e < 4; ++e) {
             const int i = 16 * w + 4 * gr + e;
             const float d = i >= j ? decay<E>((float)(mine[e] - theirs)) : 0.0f;
-            A[i * kLd + j] = i > j ? betas[i] * d * kk[ct][e] : 0.0f;
+            const float aij = i > j ? betas[i] * d * kk[ct][e] : 0.0f;
+            A[i * kLd + j] = aij;
             P[i * kLd + j] = i >= j ? d * qk[ct][e] : 0.0f;
+            if (!(__builtin_fabsf(aij) < INFINITY)) broken = 1;
         }
     }
     __syncthreads();
+    if (broken) {                                     // (the same for all)
+        // Row by row, a lane a column, over what is there alone: a row takes what is not finite from itself and rows before it.  (Products of whole blocks
+        // would carry it, times zeros, to the others.)
+        if (w == 0)
+            for (int i = 0; i < kChunk; ++i) {
+                float s = i == lane ? 1.0f : 0.0f;
+                for (int m = 0; m < i; ++m) {
+                    const float t = A[i * kLd + m] * A[m * kLd + lane];
+                    if (m >= lane) s -= t;
+                }
+                __builtin_amdgcn_wave_barrier();      // (all lanes have read the row that they replace)
+                A[i * kLd + lane] = s;
+                __builtin_amdgcn_wave_barrier();
+            }
+        __syncthreads();
+    } else {
     {                                                 // the diagonal's blocks
         float *blk = A + 16 * w * (kLd + 1), x[16];
 #pragma unroll
@@ -210,6 +230,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
         block_put(block(2 + xi, bj), x, -1.0f);
     }
     __syncthreads();
+    }
     constexpr int TRI = tri_bytes<E>(), KINDS = GRAD ? 3 : 2;
     char *out = tri + (head * chunks + c) * (int64_t)(KINDS * TRI);
     for (int f = w; f < KINDS * kFrags; f += 4) {
@@ -224,9 +245,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(E) =
             if (kind == 0) {
                 const float *bt = betas + 32 * kb + 4 * gr;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    lo[e] *= bt[e];
-                    hi[e] *= bt[16 + e];
+                for (int e = 0; e < 4; ++e) {         // (zeros stay zeros whatever beta is)
+                    const int below = 16 * rt + l - (32 * kb + 4 * gr + e);
+                    lo[e] = below >= 0 ? lo[e] * bt[e] : 0.0f;
+                    hi[e] = below >= 16 ? hi[e] * bt[16 + e] : 0.0f;
                 }
             }
         } else {

@@ -114,6 +114,22 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
         return Frag<E>(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     const v4f zero = {0, 0, 0, 0};
+    // Of accumulators whose rows are tokens: the least of a column's numbers, and its rows from `first` on replaced
+    auto least_of_columns = [&](int first) {
+#pragma unroll
+        for (int d = 16; d < kWave; d *= 2) {
+            const int other = __shfl_xor(first, d);
+            first = first < other ? first : other;
+        }
+        return first;
+    };
+    auto keep_before = [&](v4f (&x)[4], int first, float by) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * t + 4 * gr + e >= first) x[t][e] = by;
+    };
 
     if (wave < 2 * NS) {
         float *const sp = state && (len > 0 || MODE == BACKWARD) ? state + (slot * a.Hv + h) * (int64_t)a.Dk * a.Dv : nullptr;
@@ -210,6 +226,31 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
                 for (int t = 0; t < 4; ++t) x[t] = zero;
                 tri_mul<E, false>(x, tf, n0, 0);
                 tri_mul<E, false>(x, tf, n1, 1);
+                if (MODE == FORWARD && __builtin_expect(__any(x[3][0] != x[3][0]), 0)) {
+                    // A row of N that is not finite has reached all rows of U, times zeros of T, in its column.  Again without it and the rows behind it, which are then not finite.
+                    // (All of N is still in LDS.)
+                    int first = kChunk;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const v4f a0 = m.half[0][w][t * kWave + lane], a1 = m.half[1][w][t * kWave + lane], gm = factor(0, t), v4 = widen(Tile<E, W>::column_of(vs[p], t, w));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[t][e] = (kScaled<E> ? rise * v4[e] : v4[e]) - gm[e] * (a0[e] + a1[e]);
+                            const int row = 16 * t + 4 * gr + e;
+                            if (!(__builtin_fabsf(x[t][e]) < kLimit<E>)) first = first < row ? first : row;
+                        }
+                    }
+                    first = least_of_columns(first);
+                    keep_before(x, first, 0.0f);
+                    const Pieces<E> m0 = split<E>(x[0], x[1]), m1 = split<E>(x[2], x[3]);
+                    tri_read(0);
+                    tri_read(1);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) x[t] = zero;
+                    tri_mul<E, false>(x, tf, m0, 0);
+                    tri_mul<E, false>(x, tf, m1, 1);
+                    keep_before(x, first, __builtin_nanf(""));
+                }
 #pragma unroll
                 for (int t = 0; t < 4; ++t) f1[t] = factor(1, t);
 #pragma unroll
@@ -306,15 +347,42 @@ void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
             v4f y[2], old[2];
             auto finish = [&](int i) {                // O of chunk i, of which `old` is exp(G) Q S
                 const v4f *const uc = xu[i & 1] + w * XU + lane;
-                const Pieces<E> u0 = split<E>(uc[0], uc[kWave]), u1 = split<E>(uc[2 * kWave], uc[3 * kWave]);
+                const v4f was[2] = {old[0], old[1]};
+                auto add = [&](const Pieces<E> &u0, const Pieces<E> &u1) {
 #pragma unroll
-                for (int n = NP - 1; n >= 0; --n)
+                    for (int n = NP - 1; n >= 0; --n)
 #pragma unroll
-                    for (int m = 0; m <= n; ++m) {
-                        old[0] = Mx<E>::mma(old[0], u0.p[n - m], pf[0].p[m]);
-                        old[1] = Mx<E>::mma(old[1], u0.p[n - m], pf[1].p[m]);
-                        old[1] = Mx<E>::mma(old[1], u1.p[n - m], pf[2].p[m]);
+                        for (int m = 0; m <= n; ++m) {
+                            old[0] = Mx<E>::mma(old[0], u0.p[n - m], pf[0].p[m]);
+                            old[1] = Mx<E>::mma(old[1], u0.p[n - m], pf[1].p[m]);
+                            old[1] = Mx<E>::mma(old[1], u1.p[n - m], pf[2].p[m]);
+                        }
+                };
+                add(split<E>(uc[0], uc[kWave]), split<E>(uc[2 * kWave], uc[3 * kWave]));
+                const float all_of = (old[1][0] + old[1][1]) + (old[1][2] + old[1][3]);
+                if (__builtin_expect(__any(all_of != all_of), 0)) {
+                    // The same with U, whose rows that are not finite have reached all tokens, times zeros of P
+                    v4f x[4];
+                    int first = kChunk;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        x[t] = uc[t * kWave];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(__builtin_fabsf(x[t][e]) < kLimit<E>)) first = first < 16 * t + 4 * gr + e ? first : 16 * t + 4 * gr + e;
                     }
+                    first = least_of_columns(first);
+                    keep_before(x, first, 0.0f);
+                    old[0] = was[0], old[1] = was[1];
+                    add(split<E>(x[0], x[1]), split<E>(x[2], x[3]));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int from = __shfl(first, 4 * gr + e);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            if (16 * tile[t] + l >= from) old[t][e] = __builtin_nanf("");
+                    }
+                }
                 const int64_t left = a.T - (int64_t)i * kChunk, real = len - (int64_t)i * kChunk;
                 E *const oc = op + (int64_t)i * kChunk * a.o.token;
 #pragma unroll

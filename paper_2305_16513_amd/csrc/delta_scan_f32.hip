@@ -69,10 +69,33 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
     const E *const T = (const E *)ts, *const P = (const E *)ts + TRI / (int)sizeof(E);
     auto tri_frag = [&](const E *m, int at) { return get_pieces<E>(m, at); };
 
-    const int first = MODE == BACKWARD ? chunks - 1 : 0, step = MODE == BACKWARD ? -1 : 1;
-    if (chunks > 0) fetch(first);
+    // Of accumulators whose rows are tokens: the first row of the lane's column that is not finite, and rows from one on replaced
+    auto first_of = [&](const v4f (&x)[4]) {
+        int row = kChunk;
+#pragma unroll
+        for (int t = 3; t >= 0; --t)
+#pragma unroll
+            for (int e = 3; e >= 0; --e)
+                if (!(__builtin_fabsf(x[t][e]) < __builtin_inff())) row = 16 * t + 4 * gr + e;
+#pragma unroll
+        for (int d = 16; d < kWave; d *= 2) {
+            const int other = __shfl_xor(row, d);
+            row = row < other ? row : other;
+        }
+        return row;
+    };
+    auto keep_before = [&](v4f (&x)[4], int row, float by) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * t + 4 * gr + e >= row) x[t][e] = by;
+    };
+
+    const int begin = MODE == BACKWARD ? chunks - 1 : 0, step = MODE == BACKWARD ? -1 : 1;
+    if (chunks > 0) fetch(begin);
     for (int i = 0; i < chunks; ++i) {
-        const int c = first + i * step;
+        const int c = begin + i * step;
         const int64_t t0 = (int64_t)c * kChunk;
         __syncthreads();
         kr.store(ks, threadIdx.x);
@@ -112,17 +135,34 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[t][e] = vt[e] - gm[e] * x[t][e];
             }
-            const Pieces<E> n0 = split<E>(x[0], x[1]), n1 = split<E>(x[2], x[3]);
+            auto solve = [&](const v4f (&n)[4]) {     // U
+                const Pieces<E> n0 = split<E>(n[0], n[1]), n1 = split<E>(n[2], n[3]);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {             // U
-                x[t] = mma<E>(v4f{0, 0, 0, 0}, tri_frag(T, lower_at(t, 0)), n0);
-                if (t >= 2) x[t] = mma<E>(x[t], tri_frag(T, lower_at(t, 1)), n1);
+                for (int t = 0; t < 4; ++t) {
+                    x[t] = mma<E>(v4f{0, 0, 0, 0}, tri_frag(T, lower_at(t, 0)), n0);
+                    if (t >= 2) x[t] = mma<E>(x[t], tri_frag(T, lower_at(t, 1)), n1);
+                }
+            };
+            v4f n[4] = {x[0], x[1], x[2], x[3]};
+            solve(n);
+            int first = kChunk;                       // the first row of U that is not finite, of this lane's column
+            if constexpr (MODE == FORWARD) {
+                if (__any(!(__builtin_fabsf(x[3][0]) < __builtin_inff()))) {   // rows of N that are not finite have reached all of U's, times zeros of T: again without the first and those behind it
+                    const int row = first_of(n);
+                    keep_before(n, row, 0.0f);
+                    solve(n);
+                    keep_before(x, row, __builtin_nanf(""));
+                }
+                first = first_of(x);
             }
             if constexpr (MODE == KEEP) {
                 Kept<E>::put(up, 0, x[0], x[1]);
                 Kept<E>::put(up, 1, x[2], x[3]);
             } else {
-                const Pieces<E> u0 = split<E>(x[0], x[1]), u1 = split<E>(x[2], x[3]);
+                const bool some = __any(first < kChunk);
+                v4f u[4] = {x[0], x[1], x[2], x[3]};
+                if (some) keep_before(u, first, 0.0f);   // (as above, with the zeros of P)
+                const Pieces<E> u0 = split<E>(u[0], u[1]), u1 = split<E>(u[2], u[3]);
                 E *const op = o + b * a.o.batch + h * a.o.head + col0 + 16 * w + 4 * gr;
                 const int there = a.Dv - (col0 + 16 * w + 4 * gr);
 #pragma unroll
@@ -135,6 +175,10 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
                     for (int e = 0; e < 4; ++e) y[e] *= gm;
                     y = mma<E>(y, u0, tri_frag(P, lower_at(t, 0)));
                     if (t >= 2) y = mma<E>(y, u1, tri_frag(P, lower_at(t, 1)));
+                    if (some)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (16 * t + l >= __shfl(first, 4 * gr + e)) y[e] = __builtin_nanf("");
                     const int64_t token = t0 + 16 * t + l;
                     if (token < a.T && there > 0) {
                         E *p = op + token * a.o.token;
