@@ -261,7 +261,7 @@ __device__ __forceinline__ float decay(float x)
 // lie behind the end of a buffer, which loads nothing there.
 template <class E, int W, int NT, bool FULL> struct Rows {
     static constexpr int PER = 16 / (int)sizeof(E), UNITS = W / PER, N = (kChunk * UNITS + NT - 1) / NT;
-    static_assert(kChunk * UNITS % NT == 0, "whole rounds");
+    static_assert(kChunk * UNITS % NT == 0 && NT % UNITS == 0, "whole rounds of whole rows");
     v4u r[N];
 
     __device__ __forceinline__ void load(const E *p, int64_t step, int n, int width, int tid)
@@ -271,10 +271,7 @@ template <class E, int W, int NT, bool FULL> struct Rows {
             const __amdgpu_buffer_rsrc_t from = rsrc(p, n > 0 ? (unsigned)((n - 1) * st + W * (int)sizeof(E)) : 0u);
             int at = tid / UNITS * st + tid % UNITS * 16;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if constexpr (NT % UNITS == 0) r[i] = __builtin_amdgcn_raw_buffer_load_b128(from, at + i * (NT / UNITS) * st, 0, 0);
-                else r[i] = __builtin_amdgcn_raw_buffer_load_b128(from, (tid + i * NT) / UNITS * st + (tid + i * NT) % UNITS * 16, 0, 0);
-            }
+            for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(from, at + i * (NT / UNITS) * st, 0, 0);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {

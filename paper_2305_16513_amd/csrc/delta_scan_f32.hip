@@ -8,7 +8,10 @@ namespace sws {
 
 namespace {
 
-template <class E, int DK, int NW, int MODE, bool FULL>
+typedef float E;
+constexpr int NW = 2;                                 // wavefronts, 16 columns each
+
+template <int DK, int MODE, bool FULL>
 __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict__ q, const E *__restrict__ k, const E *__restrict__ v,
                                                              E *__restrict__ o, float *__restrict__ state, ScanWs ws, DeltaArgs a)
 {
@@ -265,26 +268,25 @@ __global__ __launch_bounds__(64 * NW) void delta_scan_kernel(const E *__restrict
     }
 }
 
-template <class E, int MODE>
+template <int MODE>
 hipError_t launch(const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws, const DeltaArgs &a, hipStream_t s)
 {
     const int64_t heads = a.B * a.Hv;
-    auto go = [&](auto dk, auto nw) {
-        constexpr int DK = decltype(dk)::value, NW = decltype(nw)::value;
+    auto go = [&](auto dk) {
+        constexpr int DK = decltype(dk)::value;
         // the gradients read whole blocks of 32 columns of what is kept
         const int cols = MODE == FORWARD ? a.Dv : ws.cols;
         const bool full = a.Dk == DK && a.Dv == cols && cols % (16 * NW) == 0 && full_rows<E>(a.q, DK, q) && full_rows<E>(a.k, DK, k) && full_rows<E>(a.v, 16 * NW, v) &&
                           full_rows<E>(a.o, 16 * NW, o);
-        auto *kernel = full ? delta_scan_kernel<E, DK, NW, MODE, true> : delta_scan_kernel<E, DK, NW, MODE, false>;
+        auto *kernel = full ? delta_scan_kernel<DK, MODE, true> : delta_scan_kernel<DK, MODE, false>;
         dim3 grid;
         if (!spread(heads, 64 * NW, grid, (unsigned)((cols + 16 * NW - 1) / (16 * NW)))) return kNotTaken;
         hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, s, (const E *)q, (const E *)k, (const E *)v, (E *)o, state, ws, a);
         return hipGetLastError();
     };
-    using I2 = std::integral_constant<int, 2>;
     using I64 = std::integral_constant<int, 64>;
     using I128 = std::integral_constant<int, 128>;
-    return a.Dk <= 64 ? go(I64(), I2()) : go(I128(), I2());
+    return a.Dk <= 64 ? go(I64()) : go(I128());
 }
 
 }  // namespace
@@ -292,9 +294,9 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *s
 hipError_t launch_delta_scan_f32(int mode, const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws, const DeltaArgs &a,
                                  hipStream_t s)
 {
-    if (mode == FORWARD) return launch<float, FORWARD>(q, k, v, o, state, ws, a, s);
-    if (mode == KEEP) return launch<float, KEEP>(q, k, v, o, state, ws, a, s);
-    return launch<float, BACKWARD>(q, k, v, o, state, ws, a, s);
+    if (mode == FORWARD) return launch<FORWARD>(q, k, v, o, state, ws, a, s);
+    if (mode == KEEP) return launch<KEEP>(q, k, v, o, state, ws, a, s);
+    return launch<BACKWARD>(q, k, v, o, state, ws, a, s);
 }
 
 }  // namespace sws
