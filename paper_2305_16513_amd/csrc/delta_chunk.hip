@@ -26,12 +26,12 @@ int64_t tops_size(int dtype) { return dtype == SWS_DTYPE_F16 ? 8 : 0; }
 
 // Few tokens: one after the other reads and writes the state once and needs no chunk, but takes as much time for every token, and a chunk takes as long
 // with one token as with 64.  How many are few depends on what a token costs: with few states a chain of LDS and barriers, with many the
-// arithmetic on all of them.  Bf16, states of 128 x 128, one after the other against chunks: 16 states, 8 tokens 11.2 us against 12.7, 12 tokens 15.5 against
-// 12.7; 256 states, 12 tokens 28.8 against 31.1, 16 tokens 36.4 against 31.2; 2048 states, 32 tokens 179 against 200, 48 tokens 255 against 231.
+// arithmetic on all of them.  Bf16, states of 128 x 128, one after the other against chunks: 16 states, 8 tokens 11.4 us against 15.5, 12 tokens 15.9 against
+// 15.5; 256 states, 12 tokens 29.0 against 36.3, 16 tokens 36.5 against 36.3; 2048 states, 48 tokens 255 against 278, 64 tokens 336 against 288.
 bool few(const DeltaArgs &a)
 {
     const int64_t states = a.B * a.Hv, cus = device_cus();
-    return a.T <= (states < cus ? 8 : states < 8 * cus ? 12 : 32);
+    return a.T <= (states < cus ? 8 : states < 8 * cus ? 15 : 48);
 }
 
 hipError_t launch_scan(int dtype, int mode, const void *q, const void *k, const void *v, void *o, float *state, const ScanWs &ws, const DeltaArgs &a,

@@ -76,3 +76,11 @@ def test_sizes_far_from_one(dtype, go_size, v_size, state_size, hv, dk, dv):
         fits = r.abs() < 60000
         allowed = U.HALF[got[name].dtype] * r.abs() * (1 + 2.0 ** -6) + 2e-5 * r.square().mean().sqrt() + (2.0 ** -25 if dtype == "f16" else 0)
         assert bool(((x - r).abs() <= allowed)[fits].all()), name
+
+
+@gpu
+@pytest.mark.parametrize("b,t", [(1, 8), (1, 9), (16, 15), (16, 16), (128, 48), (128, 49)])
+def test_states_on_both_sides_of_what_few_tokens_are(b, t):
+    """How many tokens are taken one by one depends on the number of states; a state's precision does not."""
+    got, want = calls(torch.Generator().manual_seed(b + t), "bf16", b, t, 16, 16, 20, 24)
+    assert off(got["state"], want["state"]) <= EXACT["state"]
