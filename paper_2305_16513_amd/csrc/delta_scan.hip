@@ -12,11 +12,13 @@
 // half of the state's rows; they exchange their halves of K S once per chunk, and both take N and U.  Two more compute, forward, O, a
 // chunk behind, from the operands of S and the accumulators of U that the first ones leave in LDS; backward, a chunk ahead, the terms with dO, which do not
 // depend on dS, and leave them as accumulators; each half of the tokens.  Four load the chunks to come and stage K, Q, V, T in LDS.  All meet
-// twice per chunk.  With Dk = 128 it takes 4700 cycles: K S 1400, N and U 1500, the update 900, meeting the others 700.  O is computed transposed, so that a lane
-// has four neighbouring elements of a token.  A workgroup has NS = 2 groups of 16 columns, or one where there are too few states to give every CU two.
+// twice per chunk.  O is computed transposed, so that a lane has four neighbouring elements of a token.  A workgroup has NS = 2 groups of 16 columns, or one where
+// there are too few states to give every CU two.
 //
-// bf16, Dk = Dv = 128: one sequence of 16384 tokens, 32 states: 395 us (256 chunks one after the other; one wavefront to 16 columns, loads by all: 495).
-// Four of 4096, 16 states each: forward 158 us; leaving states 143 us, backward 206 us (590 and 715 MB with what the gradients need: 115 and 138 us of HBM).
+// bf16, Dk = Dv = 128: one sequence of 16384 tokens, 32 states: 551 us, 256 chunks of 4500 cycles one after the other, in which a wavefront of the states issues 84 matrix
+// instructions (1340 cycles) and some 440 vector ones (1770), 264 of them to cut S, N and U into three pieces.  Counters: vector units 32 % of the
+// time, matrix units 22 %, LDS 59 %.  Four sequences of 4096, 16 states each: forward 199 us (47, 34 and 69 %); leaving states 179 us, backward 234 us (616 and 759 MB with what
+// the gradients need: 120 and 148 us of HBM).
 #include "delta.h"
 
 namespace sws {

@@ -11,8 +11,9 @@
 // 2048 columns the whole workgroup.  Column sums stay in registers over all rows of a workgroup, leave as one partial row of it and are
 // added by column_sums_kernel in a fixed order.
 //
-// [16384, 4096] bf16, x and gain there: forward 100 us for 537 MB, gradients 178 us for 805 MB (4.5 TB/s; a copy of 1 GiB: 5.2); [16384, 16 heads of 128]
-// bf16: 39 us for 201 MB, gradients 66 us for 336 MB.  Eight rows of 1800: 6 us, the launch and a read's latency.
+// [16384, 4096] bf16, x and gain there: forward 101 us for 537 MB, gradients 191 us for 805 MB (4.2 TB/s; a copy of 1 GiB: 5.1); [16384, 16 heads of 128]
+// bf16: 39 us for 201 MB, gradients 65 us for 336 MB.  Eight rows of 1800: 6 us, the launch and a read's latency.  Rows that are no multiple of eight columns, or not at multiples of 16
+// bytes, are taken element by element: [16384, 4095] 461 and 805 us, [16384, 16 heads of 127] 134 and 257 us.
 #include "seq.h"
 
 namespace sws {

@@ -7,13 +7,15 @@
 // i the head's factor:  ga = i (gy - y * sum of y gy),  gp = ga da/dp,  gx[t] = sum_j f[j] gp[t+k-1-j],  gf[j] = sum over t of gp[t] x[t-k+1+j],
 // gbias = sum of gp.
 //
-// Bound by HBM.  A lane owns eight channels (16 bytes of a 16-bit row) and a run of tokens, which slide through its registers with the
+// Forward bound by HBM, backward by its arithmetic.  A lane owns eight channels (16 bytes of a 16-bit row) and a run of tokens, which slide through its registers with the
 // taps, so that a token is read once per run; the k - 1 tokens that two runs share come from the caches.  A head's sum of squares goes across the
 // lanes that hold it (a power of two of them, idle ones among them where a head has fewer groups of eight).  The backward pass computes p
 // again instead of reading it.  Sums over tokens leave as one partial row per run and are added in a fixed order.
 //
-// [4, 4096, 6144] bf16, four taps, 4096 channels in heads of 128 to length one: forward 88 us for 403 MB (4.6 TB/s; a copy of 1 GiB: 5.2), gradients 189 us
-// for 604 MB: a head's two sums and eight sigmoids' slopes per token, 214 registers, two workgroups on a CU.  64 sequences' single tokens: 8 us, the launch and latency.
+// [4, 4096, 6144] bf16, four taps, 4096 channels in heads of 128 to length one: forward 94 us for 403 MB (4.3 TB/s; a copy of 1 GiB: 5.1), vector units busy for 69 % of them;
+// gradients 206 us for 604 MB, arithmetic more than memory: a head's two sums, eight sigmoids and their slopes per token keep the vector units busy for 68 % of the time, with 1.6
+// wavefronts on a SIMD (214 registers, two workgroups on a CU).  64 sequences' single tokens: 7 us, the launch and latency.  Rows that are no multiple of eight channels, or not at
+// multiples of 16 bytes, are taken element by element: 6143 channels, none normed, 241 and 324 us (6144: 92 and 149).
 #include "seq.h"
 
 namespace sws {
@@ -313,7 +315,7 @@ hipError_t by_taps(int k, F &&f)
 // Heads of `unit` channels (0: none are normed, and channels lie side by side: 512 of them are then a wavefront's) and runs of tokens, of which `slots`
 // workgroups a CU are at work at once: a run costs its tokens and some eight more (those that it shares with its neighbours, the taps, what a workgroup takes to start),
 // and a last round of few workgroups as much as a full one ([4, 4096, 6144], gradients: 768 workgroups of 64 tokens, two rounds on 512 places, 198 us; 492 of 100 tokens, one
-// round, 189 us).
+// round, 189 us; shortest runs of both).
 // No run is shorter than 8 unless it is the only one: the context, which the first run replaces, is then no other run's to read (k <= 8).
 void plan(ShortConvArgs &a, int unit, int unit_channels, int slots)
 {
