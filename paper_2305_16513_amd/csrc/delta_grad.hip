@@ -116,7 +116,9 @@ void delta_grad_kernel(const E *__restrict__ q, const E *__restrict__ k, const E
         const int h = hk * share + hs;
         int lane, l, gr, mine;                        // mine: token of the wavefront's own tile
         Keys ak(tid);
-        auto whereabouts = [&]() {                    // not known to be what they were before: addresses are not kept in registers until they are needed
+        // Not known to be what they were before: addresses are not kept in registers until they are needed.  (With more of them than registers, the compiler has copied one where the lanes
+        // of rows that are not there were switched off, behind the loads of the others, and left theirs behind.)
+        auto whereabouts = [&]() {
             asm volatile("" : "+v"(tid));
             lane = tid % kWave, l = tid % 16, gr = lane / 16, mine = 16 * w + l;
             ak = Keys(tid);
